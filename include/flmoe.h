@@ -368,6 +368,75 @@ int fl_moe_combine_send(fl_moe_ctx *ctx, int rank_begin, int rank_count, const v
 int fl_moe_combine_reduce(fl_moe_ctx *ctx, int rank_begin, int rank_count, const float *weights,
                           void *out, void *stream);
 
+/* ---------------------------------------------------------------- the experts' products
+ * What stands between fl_moe_dispatch_recv and fl_moe_combine_send: the experts' feed-forward block on the
+ * expert-major rows, forward and backward, and forward in e4m3 blocks.
+ *
+ * Like fl_moe_layout_static these calls take the configuration and no context: they keep nothing and use no workspace
+ * (so any number of them may run at once, from any thread, on any stream), and only enqueue kernels.
+ * They act for ranks [rank_begin, rank_begin + rank_count).  Rows are where the step's tables say: rank d's local
+ * expert j has rows [expert_off[d][j], expert_off[d][j] + tokens_per_expert[d][j]) of its rank's expert_capacity_rows
+ * rows.  expert_off [N][E/N+1] and tokens_per_expert [N][E/N] are int32 device tables: those of fl_moe_layout's view,
+ * of fl_moe_layout_static, or copies of them (a backward pass that comes after another layer's layout call needs
+ * copies).  They are read on the device: no row outside a rank's capacity is ever touched, whatever they hold.  An
+ * expert may have any number of rows, none included.  Padding rows and rows behind the last expert's are not read for
+ * any result, and not written.
+ * Rows are [N][expert_capacity_rows][width], weights [E][out][in] (expert e = d * E/N + j), all contiguous, bf16 unless
+ * said otherwise, 16-byte aligned; widths are 8..2^20 and multiples of 8, of 128 where they hold e4m3 blocks
+ * (FL_ERR_ALIGNMENT).  An output may not overlap an input, except where said.
+ * Products are summed in fp32 (the order is the kernel's own, the same from run to run) and rounded once. */
+#define FL_ACT_SILU 0 /* v / (1 + e^-v)                                              */
+#define FL_ACT_GELU 1 /* its tanh form: v / (1 + e^(-2 sqrt(2/pi) (v + 0.044715 v^3))) */
+
+/* h = act(x Wg^T) * (x Wu^T): both projections, activation and product in one kernel.
+ * x [N][cap][hidden], w [E][2 * inter][hidden]: Wg, then Wu; h [N][cap][inter].
+ * pre (may be NULL): keeps both pre-activations x Wg^T, x Wu^T for the backward pass, [N][cap][2 * inter]: bf16, or with
+ * pre_scales (fp32 [N][cap][2 * inter / 128], needs inter % 128 == 0) e4m3 codes in blocks of 128 by the rule of
+ * FL_DTYPE_E4M3_BLOCK128, half the memory.  h does not depend on how they are kept. */
+int fl_moe_expert_gated(const fl_moe_config *cfg /*host*/, int rank_begin, int rank_count, const int32_t *expert_off,
+                        const int32_t *tokens_per_expert, int inter, int activation, const void *x, const void *w,
+                        void *h, void *pre, float *pre_scales, void *stream);
+
+/* Its gradients from dh [N][cap][inter] and what fl_moe_expert_gated kept (pre, pre_scales as there).
+ *   dpre [N][cap][2 * inter] bf16: the pre-activations' gradients, dh * u * act'(g) and dh * act(g); always written, the
+ *        products below read it.  With bf16 pre it may be pre itself.
+ *   dx   [N][cap][hidden] = dpre W                    (NULL: not wanted; needs w)
+ *   dw   [E][2 * inter][hidden] = dpre^T x per expert  (NULL: not wanted; needs x); zeros for an expert without rows
+ *   h    [N][cap][inter] = act(g) * u from the kept values (NULL: not wanted): the input of the product behind, for its
+ *        weight gradient, where the caller did not keep it. */
+int fl_moe_expert_gated_backward(const fl_moe_config *cfg /*host*/, int rank_begin, int rank_count,
+                                 const int32_t *expert_off, const int32_t *tokens_per_expert, int inter, int activation,
+                                 const void *x, const void *w, const void *pre, const float *pre_scales, const void *dh,
+                                 void *dpre, void *dx, void *dw, void *h, void *stream);
+
+/* y = x W^T per expert: x [N][cap][in], w [E][out][in], y [N][cap][out] (in = inter, out = hidden behind
+ * fl_moe_expert_gated: what fl_moe_combine_send takes). */
+int fl_moe_expert_product(const fl_moe_config *cfg /*host*/, int rank_begin, int rank_count, const int32_t *expert_off,
+                          const int32_t *tokens_per_expert, int in, int out, const void *x, const void *w, void *y,
+                          void *stream);
+
+/* dx [N][cap][in] = dy W (NULL: not wanted; needs w), dw [E][out][in] = dy^T x per expert (NULL: not wanted; needs x;
+ * zeros for an expert without rows); one of the two at least. */
+int fl_moe_expert_product_backward(const fl_moe_config *cfg /*host*/, int rank_begin, int rank_count,
+                                   const int32_t *expert_off, const int32_t *tokens_per_expert, int in, int out,
+                                   const void *x, const void *w, const void *dy, void *dx, void *dw, void *stream);
+
+/* The gated block on e4m3 rows, as an e4m3 dispatch delivers them: x codes [N][cap][hidden], x_scales fp32
+ * [N][cap][hidden / 128]; w codes [E][2 * inter][hidden] with one scale per 128 x 128 block, w_scales fp32
+ * [E][2 * inter / 128][hidden / 128].  h is answered in e4m3 blocks of 128, quantised from the fp32 result by the rule of
+ * FL_DTYPE_E4M3_BLOCK128: codes [N][cap][inter], h_scales [N][cap][inter / 128].
+ * Every block's codes are multiplied and summed as they are, and the sum enters an fp32 accumulator times both scales. */
+int fl_moe_expert_gated_e4m3(const fl_moe_config *cfg /*host*/, int rank_begin, int rank_count, const int32_t *expert_off,
+                             const int32_t *tokens_per_expert, int inter, int activation, const void *x,
+                             const float *x_scales, const void *w, const float *w_scales, void *h, float *h_scales,
+                             void *stream);
+
+/* y = x W^T per expert on e4m3 rows: x codes [N][cap][in] and x_scales [N][cap][in / 128], w codes [E][out][in] and
+ * w_scales [E][ceil(out / 128)][in / 128], y bf16 [N][cap][out] (out a multiple of 8). */
+int fl_moe_expert_product_e4m3(const fl_moe_config *cfg /*host*/, int rank_begin, int rank_count, const int32_t *expert_off,
+                               const int32_t *tokens_per_expert, int in, int out, const void *x, const float *x_scales,
+                               const void *w, const float *w_scales, void *y, void *stream);
+
 /* Reads and clears the device status word (synchronises the stream). */
 int fl_moe_status(fl_moe_ctx *ctx, int32_t *host_out /*host*/, void *stream);
 

@@ -7,7 +7,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(CSRC, "libflmoe.so")
 SOURCES = ["flmoe.hip"]
-HEADERS = ["common.h", "kernels_layout.h", "kernels_shuffle.h", "../../include/flmoe.h"]
+HEADERS = ["common.h", "kernels_layout.h", "kernels_shuffle.h", "kernels_experts.h", "experts.h", "../../include/flmoe.h"]
 
 
 def lib_path() -> str:

@@ -1,0 +1,208 @@
+// Host side of the experts' products: argument checks and launches.  No context, no workspace, nothing kept.
+// (Part of flmoe.hip.)
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <atomic>
+#include <initializer_list>
+
+#include "../../include/flmoe.h"
+#include "kernels_experts.h"
+
+namespace flmoe {
+namespace experts {
+
+constexpr int kMaxWidth = 1 << 20;             // as fl_moe_config.hidden
+constexpr int kUnits = 256;                    // compute units of the part
+
+// What a call's configuration and tables come to.
+inline int groups_of(const fl_moe_config *cfg, int rank_begin, int rank_count, const int32_t *expert_off,
+              const int32_t *tokens_per_expert, Groups *G) {
+    fl_moe_sizes sizes;
+    const int e = fl_moe_query_sizes(cfg, &sizes);
+    if (e != FL_OK) return e;
+    if (rank_begin < 0 || rank_count < 1 || rank_count > cfg->n_ranks - rank_begin) return FL_ERR_INVALID_ARG;
+    if (!expert_off || !tokens_per_expert) return FL_ERR_INVALID_ARG;
+    if (((uintptr_t)expert_off & 3) || ((uintptr_t)tokens_per_expert & 3)) return FL_ERR_ALIGNMENT;
+    const int El = cfg->n_experts / cfg->n_ranks;
+    *G = Groups{El, rank_begin * El, rank_count * El, sizes.expert_capacity_rows, expert_off, tokens_per_expert};
+    return FL_OK;
+}
+
+inline int check_width(int width, int multiple) {
+    if (width < 1 || width > kMaxWidth) return FL_ERR_INVALID_ARG;
+    return width % multiple ? FL_ERR_ALIGNMENT : FL_OK;
+}
+
+// Every pointer there and 16-byte aligned (scales: 4).
+inline int check_tensors(std::initializer_list<const void *> rows, std::initializer_list<const float *> scales = {}) {
+    for (const void *p : rows) if (!p) return FL_ERR_INVALID_ARG;
+    for (const float *p : scales) if (!p) return FL_ERR_INVALID_ARG;
+    for (const void *p : rows) if ((uintptr_t)p & 15) return FL_ERR_ALIGNMENT;
+    for (const float *p : scales) if ((uintptr_t)p & 3) return FL_ERR_ALIGNMENT;
+    return FL_OK;
+}
+
+inline int compute_units() {
+    static std::atomic<int> known[64];
+    int dev = 0, n = 0;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return kUnits;
+    n = known[dev].load(std::memory_order_relaxed);
+    if (n == 0) {
+        if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n < 1) n = kUnits;
+        known[dev].store(n, std::memory_order_relaxed);
+    }
+    return n;
+}
+
+inline int launched() { return hipGetLastError() == hipSuccess ? FL_OK : FL_ERR_HIP; }
+
+template <int FORM, bool E4M3, bool GATED>
+int launch_tiles(const Groups &G, const Product &P, hipStream_t st) {
+    const int grid = std::max(1, compute_units() / kXcds) * kXcds;
+    expert_tiles_kernel<FORM, E4M3, GATED, 256, 1><<<dim3(grid), dim3(kThreads), 0, st>>>(G, P);
+    return launched();
+}
+
+// y = x W^T, W [experts][out][in]
+inline Product forward(const void *x, const void *w, void *y, int in, int out) {
+    Product P = {};
+    P.a = (const char *)w; P.b = (const char *)x; P.out = y;
+    P.a_ld = P.b_ld = 2 * in;
+    P.a_expert = (long long)out * in * 2;
+    P.features = out; P.k = in;
+    return P;
+}
+// dx = dy W
+inline Product row_gradient(const void *dy, const void *w, void *dx, int in, int out) {
+    Product P = {};
+    P.a = (const char *)w; P.b = (const char *)dy; P.out = dx;
+    P.a_ld = 2 * in; P.b_ld = 2 * out;
+    P.a_expert = (long long)out * in * 2;
+    P.features = in; P.k = out;
+    return P;
+}
+// dW = dy^T x
+inline Product weight_gradient(const void *dy, const void *x, void *dw, int in, int out) {
+    Product P = {};
+    P.a = (const char *)x; P.b = (const char *)dy; P.out = dw;
+    P.a_ld = 2 * in; P.b_ld = 2 * out;
+    P.features = in; P.other = out;
+    return P;
+}
+
+#define FL_CHECK(call) do { const int code = (call); if (code != FL_OK) return code; } while (0)
+
+}  // namespace experts
+}  // namespace flmoe
+
+extern "C" {
+
+int fl_moe_expert_gated(const fl_moe_config *cfg, int rb, int rc, const int32_t *expert_off, const int32_t *tokens_per_expert,
+                        int inter, int activation, const void *x, const void *w, void *h, void *pre, float *pre_scales,
+                        void *stream) {
+    using namespace flmoe::experts;
+    Groups G;
+    FL_CHECK(groups_of(cfg, rb, rc, expert_off, tokens_per_expert, &G));
+    FL_CHECK(check_width(inter, pre_scales ? 128 : 8));
+    if (activation != FL_ACT_SILU && activation != FL_ACT_GELU) return FL_ERR_INVALID_ARG;
+    if (pre_scales && !pre) return FL_ERR_INVALID_ARG;
+    FL_CHECK(check_tensors({x, w, h}));
+    if (((uintptr_t)pre & 15) || ((uintptr_t)pre_scales & 3)) return FL_ERR_ALIGNMENT;
+    Product P = forward(x, w, h, cfg->hidden, inter);
+    P.a_expert *= 2;
+    P.pre = pre; P.pre_scales = pre_scales; P.act = activation;
+    return launch_tiles<kForward, false, true>(G, P, (hipStream_t)stream);
+}
+
+int fl_moe_expert_gated_backward(const fl_moe_config *cfg, int rb, int rc, const int32_t *expert_off,
+                                 const int32_t *tokens_per_expert, int inter, int activation, const void *x, const void *w,
+                                 const void *pre, const float *pre_scales, const void *dh, void *dpre, void *dx, void *dw,
+                                 void *h, void *stream) {
+    using namespace flmoe::experts;
+    Groups G;
+    FL_CHECK(groups_of(cfg, rb, rc, expert_off, tokens_per_expert, &G));
+    FL_CHECK(check_width(inter, pre_scales ? 128 : 8));
+    if (activation != FL_ACT_SILU && activation != FL_ACT_GELU) return FL_ERR_INVALID_ARG;
+    FL_CHECK(check_tensors({pre, dh, dpre}));
+    if ((dx && !w) || (dw && !x) || (pre_scales && dpre == pre)) return FL_ERR_INVALID_ARG;
+    if (((uintptr_t)x | (uintptr_t)w | (uintptr_t)dx | (uintptr_t)dw | (uintptr_t)h) & 15 || (uintptr_t)pre_scales & 3)
+        return FL_ERR_ALIGNMENT;
+    hipStream_t st = (hipStream_t)stream;
+    const long long mean = std::max(1ll, (long long)cfg->max_tokens * cfg->top_k / G.El);       // rows of an expert
+    const long long blocks = std::min(std::max(1ll, (mean * (inter / 8) + 1023) / 1024), (1ll << 18) / G.n);
+    expert_gated_gradient_kernel<<<dim3((unsigned)blocks, G.n), dim3(256), 0, st>>>(
+        G, inter, activation, (const char *)pre, pre_scales, (const char *)dh, (char *)dpre, (char *)h);
+    FL_CHECK(launched());
+    if (dx) FL_CHECK((launch_tiles<kRowGradient, false, false>(G, row_gradient(dpre, w, dx, cfg->hidden, 2 * inter), st)));
+    if (dw) FL_CHECK((launch_tiles<kWeightGradient, false, false>(G, weight_gradient(dpre, x, dw, cfg->hidden, 2 * inter), st)));
+    return FL_OK;
+}
+
+int fl_moe_expert_product(const fl_moe_config *cfg, int rb, int rc, const int32_t *expert_off, const int32_t *tokens_per_expert,
+                          int in, int out, const void *x, const void *w, void *y, void *stream) {
+    using namespace flmoe::experts;
+    Groups G;
+    FL_CHECK(groups_of(cfg, rb, rc, expert_off, tokens_per_expert, &G));
+    FL_CHECK(check_width(in, 8));
+    FL_CHECK(check_width(out, 8));
+    FL_CHECK(check_tensors({x, w, y}));
+    return launch_tiles<kForward, false, false>(G, forward(x, w, y, in, out), (hipStream_t)stream);
+}
+
+int fl_moe_expert_product_backward(const fl_moe_config *cfg, int rb, int rc, const int32_t *expert_off,
+                                   const int32_t *tokens_per_expert, int in, int out, const void *x, const void *w,
+                                   const void *dy, void *dx, void *dw, void *stream) {
+    using namespace flmoe::experts;
+    Groups G;
+    FL_CHECK(groups_of(cfg, rb, rc, expert_off, tokens_per_expert, &G));
+    FL_CHECK(check_width(in, 8));
+    FL_CHECK(check_width(out, 8));
+    FL_CHECK(check_tensors({dy}));
+    if ((!dx && !dw) || (dx && !w) || (dw && !x)) return FL_ERR_INVALID_ARG;
+    if (((uintptr_t)x | (uintptr_t)w | (uintptr_t)dx | (uintptr_t)dw) & 15) return FL_ERR_ALIGNMENT;
+    hipStream_t st = (hipStream_t)stream;
+    if (dx) FL_CHECK((launch_tiles<kRowGradient, false, false>(G, row_gradient(dy, w, dx, in, out), st)));
+    if (dw) FL_CHECK((launch_tiles<kWeightGradient, false, false>(G, weight_gradient(dy, x, dw, in, out), st)));
+    return FL_OK;
+}
+
+int fl_moe_expert_gated_e4m3(const fl_moe_config *cfg, int rb, int rc, const int32_t *expert_off,
+                             const int32_t *tokens_per_expert, int inter, int activation, const void *x, const float *x_scales,
+                             const void *w, const float *w_scales, void *h, float *h_scales, void *stream) {
+    using namespace flmoe::experts;
+    Groups G;
+    FL_CHECK(groups_of(cfg, rb, rc, expert_off, tokens_per_expert, &G));
+    FL_CHECK(check_width(inter, 128));
+    FL_CHECK(check_width(cfg->hidden, 128));
+    if (activation != FL_ACT_SILU && activation != FL_ACT_GELU) return FL_ERR_INVALID_ARG;
+    FL_CHECK(check_tensors({x, w, h}, {x_scales, w_scales, h_scales}));
+    Product P = {};
+    P.a = (const char *)w; P.b = (const char *)x; P.a_scales = w_scales; P.b_scales = x_scales;
+    P.out = h; P.out_scales = h_scales; P.act = activation;
+    P.a_ld = P.b_ld = P.k = cfg->hidden;
+    P.features = inter;
+    P.a_expert = 2ll * inter * cfg->hidden;
+    return launch_tiles<kForward, true, true>(G, P, (hipStream_t)stream);
+}
+
+int fl_moe_expert_product_e4m3(const fl_moe_config *cfg, int rb, int rc, const int32_t *expert_off,
+                               const int32_t *tokens_per_expert, int in, int out, const void *x, const float *x_scales,
+                               const void *w, const float *w_scales, void *y, void *stream) {
+    using namespace flmoe::experts;
+    Groups G;
+    FL_CHECK(groups_of(cfg, rb, rc, expert_off, tokens_per_expert, &G));
+    FL_CHECK(check_width(in, 128));
+    FL_CHECK(check_width(out, 8));
+    FL_CHECK(check_tensors({x, w, y}, {x_scales, w_scales}));
+    Product P = {};
+    P.a = (const char *)w; P.b = (const char *)x; P.a_scales = w_scales; P.b_scales = x_scales;
+    P.out = y;
+    P.a_ld = P.b_ld = P.k = in;
+    P.features = out;
+    P.a_expert = (long long)out * in;
+    return launch_tiles<kForward, true, false>(G, P, (hipStream_t)stream);
+}
+
+}  // extern "C"

@@ -1155,3 +1155,5 @@ const char *fl_moe_kernel_name(int kernel_id) {
 }
 
 }  // extern "C"
+
+#include "experts.h"

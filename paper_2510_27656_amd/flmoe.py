@@ -23,6 +23,7 @@ FL_FLAG_STREAM_ORDERED = 2
 FL_FLAG_PEER_PUSH = 4
 FL_FLAG_PARTIAL_SUMS = 8
 FL_FLAG_PROGRESSIVE_RECV = 16
+FL_ACT_SILU, FL_ACT_GELU = 0, 1
 FL_KERNEL_COUNT = 11
 
 
@@ -83,7 +84,8 @@ EXPORTS = ["fl_moe_query_sizes", "fl_moe_create", "fl_moe_destroy", "fl_moe_layo
            "fl_moe_dispatch_send", "fl_moe_dispatch_send_weighted", "fl_moe_dispatch_send_e4m3",
            "fl_moe_dispatch_recv",
            "fl_moe_combine_send",
-           "fl_moe_combine_reduce", "fl_moe_status", "fl_moe_reset", "fl_moe_required_capacities",
+           "fl_moe_combine_reduce", "fl_moe_expert_gated", "fl_moe_expert_gated_backward", "fl_moe_expert_product",
+           "fl_moe_expert_product_backward", "fl_moe_expert_gated_e4m3", "fl_moe_expert_product_e4m3", "fl_moe_status", "fl_moe_reset", "fl_moe_required_capacities",
            "fl_moe_strerror", "fl_moe_debug_views", "fl_moe_debug_row_strides",
            "fl_moe_debug_tune", "fl_moe_debug_launch_groups", "fl_moe_debug_launch_plan", "fl_moe_debug_ordering_plan",
            "fl_moe_debug_copy", "fl_moe_debug_fill", "fl_moe_debug_read", "fl_moe_profile_enable", "fl_moe_profile_collect", "fl_moe_profile_read",
@@ -120,6 +122,13 @@ def lib():
         L.fl_moe_dispatch_recv.argtypes = [vp, i32, i32, vp, vp, vp, vp]
         L.fl_moe_combine_send.argtypes = [vp, i32, i32, vp, vp]
         L.fl_moe_combine_reduce.argtypes = [vp, i32, i32, vp, vp, vp]
+        rows = [C.POINTER(fl_moe_config), i32, i32, vp, vp, i32, i32]      # ..., widths or width and activation
+        L.fl_moe_expert_gated.argtypes = rows + [vp] * 6
+        L.fl_moe_expert_gated_backward.argtypes = rows + [vp] * 10
+        L.fl_moe_expert_product.argtypes = rows + [vp] * 4
+        L.fl_moe_expert_product_backward.argtypes = rows + [vp] * 6
+        L.fl_moe_expert_gated_e4m3.argtypes = rows + [vp] * 7
+        L.fl_moe_expert_product_e4m3.argtypes = rows + [vp] * 6
         L.fl_moe_status.argtypes = [vp, C.POINTER(C.c_int32), vp]
         L.fl_moe_reset.argtypes = [vp, vp]
         L.fl_moe_required_capacities.argtypes = [vp, C.POINTER(C.c_int64), C.POINTER(C.c_int64), vp]
@@ -244,6 +253,104 @@ def fl_moe_combine_send(ctx, rank_begin, rank_count, expert_y, stream=None):
 def fl_moe_combine_reduce(ctx, rank_begin, rank_count, weights, out, stream=None):
     _check(lib().fl_moe_combine_reduce(ctx, rank_begin, rank_count, _ptr(weights), _ptr(out),
                                        _stream(stream)), "fl_moe_combine_reduce")
+
+
+# The experts' products take tensors of many shapes, so their types and sizes are checked here as well: the library
+# sees addresses only.
+_BF16, _F32, _I32 = (torch.bfloat16,), (torch.float32,), (torch.int32,)
+_E4M3 = (torch.uint8, torch.float8_e4m3fn)
+
+
+class _Tensors:
+    """Addresses of one call's tensors; each of the given type, of at least so many elements, on the current device."""
+
+    def __init__(self, cfg, where):
+        self.where = where
+        self.sizes = fl_moe_query_sizes(cfg)
+        self.rows = cfg.n_ranks * self.sizes.expert_capacity_rows
+        self.experts, self.ranks = cfg.n_experts, cfg.n_ranks
+
+    def __call__(self, t, dtypes, count, optional=False):
+        if t is None and optional:
+            return None
+        if (not isinstance(t, torch.Tensor) or not t.is_cuda or t.get_device() != _current_device() or t.dtype not in dtypes
+                or t.numel() < count or not t.is_contiguous()):
+            raise FlMoeError(FL_ERR_INVALID_ARG, f"{self.where}: a tensor of {count} or more {dtypes[0]} elements in a row on "
+                             f"the current device is needed, got {_described(t)}")
+        return t.data_ptr()
+
+    def tables(self, expert_off, tokens_per_expert):
+        if isinstance(expert_off, int) and isinstance(tokens_per_expert, int):      # of a fl_moe_layout_view
+            return expert_off, tokens_per_expert
+        return self(expert_off, _I32, self.experts + self.ranks), self(tokens_per_expert, _I32, self.experts)
+
+
+def _described(t):
+    return f"{t.dtype} {tuple(t.shape)} on {t.device}" if isinstance(t, torch.Tensor) else repr(t)
+
+
+def fl_moe_expert_gated(cfg, rank_begin, rank_count, expert_off, tokens_per_expert, inter, activation, x, w, h, pre=None,
+                        pre_scales=None, stream=None):
+    t = _Tensors(cfg, "fl_moe_expert_gated")
+    _check(lib().fl_moe_expert_gated(
+        C.byref(cfg), rank_begin, rank_count, *t.tables(expert_off, tokens_per_expert), inter, activation,
+        t(x, _BF16, t.rows * cfg.hidden), t(w, _BF16, t.experts * 2 * inter * cfg.hidden), t(h, _BF16, t.rows * inter),
+        t(pre, _BF16 if pre_scales is None else _E4M3, t.rows * 2 * inter, True),
+        t(pre_scales, _F32, t.rows * 2 * inter // 128, True), _stream(stream)), t.where)
+
+
+def fl_moe_expert_gated_backward(cfg, rank_begin, rank_count, expert_off, tokens_per_expert, inter, activation, x, w, pre,
+                                 pre_scales, dh, dpre, dx=None, dw=None, h=None, stream=None):
+    t = _Tensors(cfg, "fl_moe_expert_gated_backward")
+    weights = t.experts * 2 * inter * cfg.hidden
+    _check(lib().fl_moe_expert_gated_backward(
+        C.byref(cfg), rank_begin, rank_count, *t.tables(expert_off, tokens_per_expert), inter, activation,
+        t(x, _BF16, t.rows * cfg.hidden, True), t(w, _BF16, weights, True),
+        t(pre, _BF16 if pre_scales is None else _E4M3, t.rows * 2 * inter),
+        t(pre_scales, _F32, t.rows * 2 * inter // 128, True), t(dh, _BF16, t.rows * inter),
+        t(dpre, _BF16, t.rows * 2 * inter), t(dx, _BF16, t.rows * cfg.hidden, True), t(dw, _BF16, weights, True),
+        t(h, _BF16, t.rows * inter, True), _stream(stream)), t.where)
+
+
+def fl_moe_expert_product(cfg, rank_begin, rank_count, expert_off, tokens_per_expert, in_features, out_features, x, w, y,
+                          stream=None):
+    t = _Tensors(cfg, "fl_moe_expert_product")
+    _check(lib().fl_moe_expert_product(
+        C.byref(cfg), rank_begin, rank_count, *t.tables(expert_off, tokens_per_expert), in_features, out_features,
+        t(x, _BF16, t.rows * in_features), t(w, _BF16, t.experts * in_features * out_features),
+        t(y, _BF16, t.rows * out_features), _stream(stream)), t.where)
+
+
+def fl_moe_expert_product_backward(cfg, rank_begin, rank_count, expert_off, tokens_per_expert, in_features, out_features, x,
+                                   w, dy, dx=None, dw=None, stream=None):
+    t = _Tensors(cfg, "fl_moe_expert_product_backward")
+    weights = t.experts * in_features * out_features
+    _check(lib().fl_moe_expert_product_backward(
+        C.byref(cfg), rank_begin, rank_count, *t.tables(expert_off, tokens_per_expert), in_features, out_features,
+        t(x, _BF16, t.rows * in_features, True), t(w, _BF16, weights, True), t(dy, _BF16, t.rows * out_features),
+        t(dx, _BF16, t.rows * in_features, True), t(dw, _BF16, weights, True), _stream(stream)), t.where)
+
+
+def fl_moe_expert_gated_e4m3(cfg, rank_begin, rank_count, expert_off, tokens_per_expert, inter, activation, x, x_scales, w,
+                             w_scales, h, h_scales, stream=None):
+    t = _Tensors(cfg, "fl_moe_expert_gated_e4m3")
+    weights = t.experts * 2 * inter * cfg.hidden
+    _check(lib().fl_moe_expert_gated_e4m3(
+        C.byref(cfg), rank_begin, rank_count, *t.tables(expert_off, tokens_per_expert), inter, activation,
+        t(x, _E4M3, t.rows * cfg.hidden), t(x_scales, _F32, t.rows * cfg.hidden // 128), t(w, _E4M3, weights),
+        t(w_scales, _F32, weights // (128 * 128)), t(h, _E4M3, t.rows * inter), t(h_scales, _F32, t.rows * inter // 128),
+        _stream(stream)), t.where)
+
+
+def fl_moe_expert_product_e4m3(cfg, rank_begin, rank_count, expert_off, tokens_per_expert, in_features, out_features, x,
+                               x_scales, w, w_scales, y, stream=None):
+    t = _Tensors(cfg, "fl_moe_expert_product_e4m3")
+    _check(lib().fl_moe_expert_product_e4m3(
+        C.byref(cfg), rank_begin, rank_count, *t.tables(expert_off, tokens_per_expert), in_features, out_features,
+        t(x, _E4M3, t.rows * in_features), t(x_scales, _F32, t.rows * in_features // 128),
+        t(w, _E4M3, t.experts * in_features * out_features),
+        t(w_scales, _F32, t.experts * ((out_features + 127) // 128) * (in_features // 128)),
+        t(y, _BF16, t.rows * out_features), _stream(stream)), t.where)
 
 
 def fl_moe_status(ctx, stream=None) -> int:

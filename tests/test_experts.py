@@ -1,0 +1,601 @@
+"""The experts' products (fl_moe_expert_*) against the formulas in 64 bits, and their refusals.
+
+Tolerances are bounds, derived here once.  A sum of k products in fp32, in any order, each step off by at most one unit
+in the last place (2^-23) of what has been summed: off by at most k 2^-23 sum |a b|.  A result rounded to bf16: half a
+step, 2^-8 of the value; to an e4m3 block: 2^-4 of the value or half the smallest step, 2^-10 of the scale.
+Inputs of bf16 or e4m3 are exact in 64 bits."""
+import ctypes as C
+import math
+
+import pytest
+import torch
+
+from paper_2510_27656_amd import flmoe
+
+U = 2.0 ** -23
+BF16 = 2.0 ** -8
+TINY = 2.0 ** -120           # below it bf16 and fp32 have subnormal steps; no value tested lies there
+SLOPE = 1.2                  # no activation here is steeper (silu 1.0999, gelu 1.1289)
+
+
+def config(counts, hidden=256, cap=0, max_tokens=None, top_k=1, align=1):
+    n, el = len(counts), len(counts[0])
+    tokens = max_tokens or max(1, max(sum(c) for c in counts))
+    return flmoe.fl_moe_config(n, n * el, tokens, top_k, hidden, 0, align, 0, 0, cap, 0, 0, 0)
+
+
+# ------------------------------------------------------------------ refusals (no GPU)
+P = 0x10000                  # an aligned address that no refused call looks at
+
+
+def calls():
+    c = config([[4, 4], [4, 4]], hidden=256)
+    at = [C.byref(c), 0, 2, P, P]
+    return {
+        "fl_moe_expert_gated": at + [128, 0] + [P, P, P, None, None, None],
+        "fl_moe_expert_gated_backward": at + [128, 0] + [P, P, P, None, P, P + 16, P, P, None, None],
+        "fl_moe_expert_product": at + [128, 256] + [P, P, P, None],
+        "fl_moe_expert_product_backward": at + [128, 256] + [P, P, P, P, P, None],
+        "fl_moe_expert_gated_e4m3": at + [128, 0] + [P, P, P, P, P, P, None],
+        "fl_moe_expert_product_e4m3": at + [128, 256] + [P, P, P, P, P, None],
+    }
+
+
+INVALID, ALIGNMENT = flmoe.FL_ERR_INVALID_ARG, flmoe.FL_ERR_ALIGNMENT
+
+
+def refused(name, code, **changed):
+    args = calls()[name]
+    for place, v in changed.items():
+        args[int(place[1:])] = v
+    assert getattr(flmoe.lib(), name)(*args) == code, changed
+
+
+@pytest.mark.parametrize("name", sorted(calls()))
+def test_ranges_tables_and_pointers_are_refused(name):
+    refused(name, INVALID, a0=None)
+    bad = config([[4, 4], [4, 4]])
+    bad.top_k = 0
+    refused(name, INVALID, a0=C.byref(bad))
+    for begin, count in ((-1, 1), (0, 0), (0, 3), (2, 1), (1, 2), (0, -1), (1, 0x7fffffff)):
+        refused(name, INVALID, a1=begin, a2=count)
+    refused(name, INVALID, a3=None)
+    refused(name, INVALID, a4=None)
+    refused(name, ALIGNMENT, a3=P + 2)
+    refused(name, ALIGNMENT, a4=P + 1)
+    refused(name, INVALID, a5=0)
+    refused(name, INVALID, a5=-8)
+    refused(name, INVALID, a5=(1 << 20) + 128)
+    refused(name, ALIGNMENT, a5=130)
+    if "product" in name:
+        refused(name, INVALID, a6=0)
+        refused(name, INVALID, a6=(1 << 20) + 8)
+        refused(name, ALIGNMENT, a6=257)
+    else:
+        refused(name, INVALID, a6=2)
+        refused(name, INVALID, a6=-1)
+
+
+@pytest.mark.parametrize("name,needed", [
+    ("fl_moe_expert_gated", (7, 8, 9)), ("fl_moe_expert_gated_backward", (9, 11, 12)), ("fl_moe_expert_product", (7, 8, 9)),
+    ("fl_moe_expert_product_backward", (9,)), ("fl_moe_expert_gated_e4m3", (7, 8, 9, 10, 11, 12)),
+    ("fl_moe_expert_product_e4m3", (7, 8, 9, 10, 11))])
+def test_missing_and_misaligned_tensors_are_refused(name, needed):
+    for place in needed:
+        refused(name, INVALID, **{f"a{place}": None})
+        refused(name, ALIGNMENT, **{f"a{place}": P + 2})
+
+
+def test_what_belongs_together_is_refused_apart():
+    refused("fl_moe_expert_gated", INVALID, a11=P)                              # scales of nothing
+    refused("fl_moe_expert_gated", ALIGNMENT, a10=P, a11=P, a5=136)             # blocks of 128 in a width of 136
+    refused("fl_moe_expert_gated", ALIGNMENT, a10=P + 8)
+    refused("fl_moe_expert_gated", ALIGNMENT, a10=P, a11=P + 1)
+    back = "fl_moe_expert_gated_backward"
+    refused(back, INVALID, a8=None)                                             # dx without w
+    refused(back, INVALID, a7=None)                                             # dw without x
+    refused(back, INVALID, a10=P, a12=P)                                        # 8-bit rows are no place for dpre
+    refused(back, ALIGNMENT, a10=P, a5=136)
+    for place in (7, 8, 13, 14, 15):
+        refused(back, ALIGNMENT, **{f"a{place}": P + 8})
+    back = "fl_moe_expert_product_backward"
+    refused(back, INVALID, a10=None, a11=None)                                  # nothing wanted
+    refused(back, INVALID, a8=None)
+    refused(back, INVALID, a7=None)
+    for place in (7, 8, 10, 11):
+        refused(back, ALIGNMENT, **{f"a{place}": P + 8})
+    refused("fl_moe_expert_gated_e4m3", ALIGNMENT, a0=C.byref(config([[4, 4], [4, 4]], hidden=264)))
+    refused("fl_moe_expert_product_e4m3", ALIGNMENT, a5=136)
+
+
+def test_the_binding_refuses_host_tensors():
+    c = config([[4, 4]])
+    z = torch.zeros(1 << 16, dtype=torch.bfloat16)
+    t = torch.zeros(8, dtype=torch.int32)
+    for call in (lambda: flmoe.fl_moe_expert_gated(c, 0, 1, t, t, 128, 0, z, z, z),
+                 lambda: flmoe.fl_moe_expert_product(c, 0, 1, t, t, 128, 256, z, z, z),
+                 lambda: flmoe.fl_moe_expert_product_backward(c, 0, 1, t, t, 128, 256, z, z, z, z)):
+        with pytest.raises(flmoe.FlMoeError) as e:
+            call()
+        assert e.value.code == INVALID
+
+
+# ------------------------------------------------------------------ on the GPU
+class Layer:
+    """Rows, tables and weights of one call.  Unused rows hold NaN: nothing may read a result out of them."""
+
+    def __init__(self, counts, hidden, seed=0, cap=None, align=1, lead=0):
+        self.counts, self.n, self.el, self.hidden = counts, len(counts), len(counts[0]), hidden
+        off = []
+        for per in counts:
+            at, row = lead, [lead]
+            for j, c in enumerate(per):
+                at += -(-c // align) * align if j + 1 < len(per) else c
+                row.append(at)
+            off.append(row)
+        self.off = off
+        need = max(max(o) for o in off)
+        self.cap = max(1, cap or need + 3)
+        # as many tokens as the capacity needs: the configuration's own bound on rows
+        self.cfg = config(counts, hidden, cap=self.cap, max_tokens=self.cap, align=1)
+        assert flmoe.fl_moe_query_sizes(self.cfg).expert_capacity_rows == self.cap
+        self.g = torch.Generator(device="cuda").manual_seed(seed)
+        self.expert_off = torch.tensor(off, dtype=torch.int32, device="cuda")
+        self.loads = torch.tensor(counts, dtype=torch.int32, device="cuda")
+        self.at = (self.cfg, 0, self.n, self.expert_off, self.loads)
+        self.used = torch.zeros((self.n, self.cap), dtype=torch.bool, device="cuda")
+        for d, j in self.experts():
+            self.used[d, self.span(d, j)] = True
+
+    def experts(self):
+        return [(d, j) for d in range(self.n) for j in range(self.el)]
+
+    def span(self, d, j):
+        return slice(self.off[d][j], self.off[d][j] + self.counts[d][j])
+
+    def randn(self, *shape, scale=1.0):
+        return (torch.randn(shape, generator=self.g, device="cuda") * scale).to(torch.bfloat16)
+
+    def rows(self, width, scale=1.0):
+        r = self.randn(self.n, self.cap, width, scale=scale)
+        r[~self.used] = math.nan
+        return r
+
+    def weights(self, out, in_):
+        return self.randn(self.n * self.el, out, in_, scale=1 / math.sqrt(in_))
+
+    def unwritten(self, width, dtype=torch.bfloat16):
+        return torch.full((self.n, self.cap, width), 77, device="cuda").to(dtype)
+
+    def check_rows(self, got, want, tolerance, what):
+        """got within the tolerance of want(d, j) on every expert's rows, and as it was elsewhere."""
+        for d, j in self.experts():
+            if self.counts[d][j]:
+                check(got[d, self.span(d, j)], want[d, j], tolerance[d, j], f"{what} of expert {d}, {j}")
+        left = got[~self.used]
+        assert bool((left == torch.full_like(left[:1], 77) if left.dtype != torch.float8_e4m3fn else left.float() == 77).all()), \
+            f"{what}: a row of no expert was written"
+
+
+def check(got, want, tolerance, what):
+    got, off = got.double(), (got.double() - want).abs()
+    bad = ~(off <= tolerance)
+    assert not bool(bad.any()), f"{what}: {int(bad.sum())} of {bad.numel()} off, the worst {float((off / tolerance).max()):.3g} times " \
+        f"the tolerance, at {bad.nonzero()[0].tolist()}: {float(got[bad][0])} for {float(want[bad][0])}"
+
+
+def act64(v, act):
+    """activation, slope, and the argument of its exponential"""
+    arg = v if act == 0 else 2 * math.sqrt(2 / math.pi) * (v + 0.044715 * v ** 3)
+    s = torch.sigmoid(arg)
+    inner = v if act == 0 else 2 * math.sqrt(2 / math.pi) * (v + 3 * 0.044715 * v ** 3)
+    return v * s, s + inner * s * (1 - s), arg
+
+
+def act_off(v, act, dv):
+    """How far the activation of v, itself off by dv, may be: the exponential is good to a few units and to its argument's
+    rounding."""
+    a, _, arg = act64(v, act)
+    return SLOPE * dv + (a.abs() + dv) * U * (16 + 8 * arg.abs())
+
+
+def gated64(x, w, act, steps=None):
+    """g, u, h and how far fp32 sums of `steps` additions leave g, u, h off, before rounding."""
+    i = w.shape[0] // 2
+    p, size = x @ w.T, x.abs() @ w.abs().T
+    dp = (steps or x.shape[1]) * U * size
+    g, u, dg, du = p[:, :i], p[:, i:], dp[:, :i], dp[:, i:]
+    a = act64(g, act)[0]
+    da = act_off(g, act, dg)
+    return p, dp, a * u, da * (u.abs() + du) + a.abs() * du + 2 * U * (a * u).abs()
+
+
+# no rows, one, fewer and more than any tile, a whole tile and its neighbours
+SHAPES = [
+    ([[1]], 8, 8), ([[3, 0]], 72, 40), ([[16, 17, 0, 1], [0, 0, 0, 0], [5, 0, 31, 33]], 256, 128),
+    ([[64, 65]], 264, 136), ([[127, 128, 129]], 520, 264), ([[255, 0, 257], [256, 2, 511]], 200, 392),
+    ([[700, 40]], 1032, 648), ([[9, 1000]], 2048, 96),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("act", [0, 1])
+@pytest.mark.parametrize("keep", ["nothing", "bf16", "e4m3"])
+@pytest.mark.parametrize("counts,hidden,inter", SHAPES)
+def test_gated(counts, hidden, inter, keep, act):
+    if keep == "e4m3":
+        inter = -(-inter // 128) * 128
+    L = Layer(counts, hidden, align=16 if len(counts) > 1 else 1)
+    x, w, h = L.rows(hidden), L.weights(2 * inter, hidden), L.unwritten(inter)
+    pre = {"nothing": None, "bf16": L.unwritten(2 * inter), "e4m3": L.unwritten(2 * inter, torch.float8_e4m3fn)}[keep]
+    scales = L.unwritten(2 * inter // 128, torch.float32) if keep == "e4m3" else None
+    if keep == "e4m3":
+        pre.view(torch.uint8).fill_(0)
+        pre.copy_(torch.full_like(pre.float(), 77).to(pre.dtype))
+    flmoe.fl_moe_expert_gated(*L.at, inter, act, x, w, h, pre, scales)
+    want, tol, kept, kept_tol = {}, {}, {}, {}
+    for d, j in L.experts():
+        p, dp, h64, dh = gated64(x[d, L.span(d, j)].double(), w[d * L.el + j].double(), act)
+        want[d, j], tol[d, j] = h64, h64.abs() * BF16 + (1 + BF16) * dh + TINY
+        kept[d, j], kept_tol[d, j] = p, p.abs() * BF16 + (1 + BF16) * dp + TINY
+    L.check_rows(h, want, tol, "h")
+    if keep == "bf16":
+        L.check_rows(pre, kept, kept_tol, "pre")
+    if keep == "e4m3":
+        check_blocks(L, pre, scales, kept, {e: t - kept[e].abs() * BF16 for e, t in kept_tol.items()}, "pre")
+
+
+def check_blocks(L, codes, scales, want, off, what):
+    """e4m3 blocks of want, itself off by `off` before it was quantised."""
+    for d, j in L.experts():
+        if not L.counts[d][j]:
+            continue
+        v, o = want[d, j].unflatten(1, (-1, 128)), off[d, j].unflatten(1, (-1, 128))
+        s = scales[d, L.span(d, j)].double()[..., None]
+        most, most_off = v.abs().amax(-1, keepdim=True), o.amax(-1, keepdim=True)
+        check(s, most / 448, most / 448 * 2 * U + most_off / 448 + 2.0 ** -149, f"scales of {what} of expert {d}, {j}")
+        got = codes[d, L.span(d, j)].float().double().unflatten(1, (-1, 128)) * s
+        # half a step of the value (or of the smallest step), of the value as it was; the largest is held at 448 scales
+        check(got, v, (v.abs() + o) * 2.0 ** -4 * (1 + 8 * U) + s * 2.0 ** -10 + o * (1 + 4 * U) + v.abs() * 4 * U + TINY, f"{what} of expert {d}, {j}")
+    left = codes.float()[~L.used]
+    assert bool((left == left[:1]).all()) and bool((scales[~L.used] == 77).all()), f"{what}: a row of no expert was written"
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("act", [0, 1])
+@pytest.mark.parametrize("kept", ["bf16", "in place", "e4m3"])
+@pytest.mark.parametrize("counts,hidden,inter", SHAPES)
+def test_gated_backward(counts, hidden, inter, kept, act):
+    """Every product against what it was given: dpre and h against pre, dx and dw against dpre."""
+    if kept == "e4m3":
+        inter = -(-inter // 128) * 128
+    L = Layer(counts, hidden, align=16 if len(counts) > 1 else 1)
+    x, w, dh = L.rows(hidden), L.weights(2 * inter, hidden), L.rows(inter)
+    p = L.rows(2 * inter, scale=3.0)
+    scales = None
+    if kept == "e4m3":
+        pre = (torch.randn(p.shape, generator=L.g, device="cuda") * 100).clamp(-448, 448).to(torch.float8_e4m3fn)
+        scales = torch.rand((L.n, L.cap, 2 * inter // 128), generator=L.g, device="cuda") / 50
+        p64 = (pre.float().double().unflatten(2, (-1, 128)) * scales.double()[..., None]).flatten(2)
+    else:
+        pre, p64 = p, p.double()
+    dpre = pre if kept == "in place" else L.unwritten(2 * inter)
+    dx, h, dw = L.unwritten(hidden), L.unwritten(inter), torch.full_like(w, 77)
+    flmoe.fl_moe_expert_gated_backward(*L.at, inter, act, x, w, pre, scales, dh, dpre, dx, dw, h)
+    want, tol = {k: {} for k in ("dpre", "dx", "h")}, {k: {} for k in ("dpre", "dx", "h")}
+    for d, j in L.experts():
+        rows, e = L.span(d, j), d * L.el + j
+        g, u = p64[d, rows, :inter], p64[d, rows, inter:]
+        up = dh[d, rows].double()
+        a, slope, arg = act64(g, act)
+        da = act_off(g, act, g.abs() * U)
+        # the slope: s and inner s (1 - s), s good to a few units and its argument's rounding
+        dslope = (U * (16 + 8 * arg.abs())) * (1 + arg.abs() * 3)
+        want["dpre"][d, j] = torch.cat((up * u * slope, up * a), 1)
+        off = torch.cat(((up * u).abs() * (dslope + 4 * U), up.abs() * (da + 4 * U * a.abs())), 1)
+        tol["dpre"][d, j] = want["dpre"][d, j].abs() * BF16 + (1 + BF16) * off + TINY
+        want["h"][d, j] = a * u
+        tol["h"][d, j] = (a * u).abs() * (BF16 + 4 * U) + (1 + BF16) * da * u.abs() + TINY
+        dp, we = dpre[d, rows].double(), w[e].double()
+        want["dx"][d, j] = dp @ we
+        tol["dx"][d, j] = want["dx"][d, j].abs() * BF16 + (1 + BF16) * 2 * inter * U * (dp.abs() @ we.abs()) + TINY
+        xe = x[d, rows].double()
+        check(dw[e], dp.T @ xe, (dp.T @ xe).abs() * BF16 + (1 + BF16) * L.counts[d][j] * U * (dp.abs().T @ xe.abs()) + TINY, f"dw of expert {e}")
+    if kept != "in place":
+        L.check_rows(dpre, want["dpre"], tol["dpre"], "dpre")
+    else:
+        for d, j in L.experts():
+            check(dpre[d, L.span(d, j)], want["dpre"][d, j], tol["dpre"][d, j], "dpre in place")
+    L.check_rows(dx, want["dx"], tol["dx"], "dx")
+    L.check_rows(h, want["h"], tol["h"], "h")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("counts,in_,out", SHAPES + [([[300]], 128, 8), ([[2, 2]], 4104, 16)])
+def test_product_and_its_gradients(counts, in_, out):
+    L = Layer(counts, 256)
+    x, w, dy = L.rows(in_), L.weights(out, in_), L.rows(out)
+    y, dx, dw = L.unwritten(out), L.unwritten(in_), torch.full_like(w, 77)
+    flmoe.fl_moe_expert_product(*L.at, in_, out, x, w, y)
+    flmoe.fl_moe_expert_product_backward(*L.at, in_, out, x, w, dy, dx, dw)
+    want, tol = {"y": {}, "dx": {}}, {"y": {}, "dx": {}}
+    for d, j in L.experts():
+        rows, e = L.span(d, j), d * L.el + j
+        xe, we, de = x[d, rows].double(), w[e].double(), dy[d, rows].double()
+        want["y"][d, j], want["dx"][d, j] = xe @ we.T, de @ we
+        tol["y"][d, j] = want["y"][d, j].abs() * BF16 + (1 + BF16) * in_ * U * (xe.abs() @ we.abs().T) + TINY
+        tol["dx"][d, j] = want["dx"][d, j].abs() * BF16 + (1 + BF16) * out * U * (de.abs() @ we.abs()) + TINY
+        check(dw[e], de.T @ xe, (de.T @ xe).abs() * BF16 + (1 + BF16) * L.counts[d][j] * U * (de.abs().T @ xe.abs()) + TINY, f"dw of expert {e}")
+    L.check_rows(y, want["y"], tol["y"], "y")
+    L.check_rows(dx, want["dx"], tol["dx"], "dx")
+    # one gradient alone is the same gradient
+    only = torch.full_like(w, 77)
+    flmoe.fl_moe_expert_product_backward(*L.at, in_, out, x, None, dy, None, only)
+    assert torch.equal(only, dw)
+    only = L.unwritten(in_)
+    flmoe.fl_moe_expert_product_backward(*L.at, in_, out, None, w, dy, only, None)
+    assert torch.equal(only, dx)
+
+
+def e4m3_rows(L, width):
+    codes = (torch.randn((L.n, L.cap, width), generator=L.g, device="cuda") * 120).clamp(-448, 448).to(torch.float8_e4m3fn)
+    scales = (torch.rand((L.n, L.cap, width // 128), generator=L.g, device="cuda") + 0.5) / 120
+    codes.view(torch.uint8)[~L.used] = 0x7f                  # NaN
+    scales[~L.used] = math.nan
+    return codes, scales
+
+
+def e4m3_weights(L, out, in_):
+    e = L.n * L.el
+    codes = (torch.randn((e, out, in_), generator=L.g, device="cuda") * 120).clamp(-448, 448).to(torch.float8_e4m3fn)
+    scales = (torch.rand((e, -(-out // 128), in_ // 128), generator=L.g, device="cuda") + 0.5) / (120 * math.sqrt(in_))
+    wide = scales.double().repeat_interleave(128, 1)[:, :out].repeat_interleave(128, 2)
+    return codes, scales, codes.float().double() * wide
+
+
+def dequantised(codes, scales):
+    return codes.float().double() * scales.double().repeat_interleave(128, -1)
+
+
+E4M3_SHAPES = [([[1]], 128, 128), ([[3, 0]], 256, 384), ([[16, 17, 0, 1], [0, 0, 0, 0], [5, 0, 31, 33]], 384, 128),
+               ([[127, 128, 129]], 512, 256), ([[255, 0, 257], [256, 2, 511]], 256, 640), ([[9, 700]], 2048, 128)]
+
+
+def sums(k):
+    """Steps of a sum over e4m3 blocks: 128 products in a block, a multiplication of the scales, one addition a block."""
+    return 128 + 3 + k // 128
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("act", [0, 1])
+@pytest.mark.parametrize("counts,hidden,inter", E4M3_SHAPES)
+def test_gated_e4m3(counts, hidden, inter, act):
+    L = Layer(counts, hidden, align=16 if len(counts) > 1 else 1)
+    (x, xs), (w, ws, w64) = e4m3_rows(L, hidden), e4m3_weights(L, 2 * inter, hidden)
+    h, hs = L.unwritten(inter, torch.uint8).view(torch.float8_e4m3fn), L.unwritten(inter // 128, torch.float32)
+    flmoe.fl_moe_expert_gated_e4m3(*L.at, inter, act, x, xs, w, ws, h, hs)
+    want, off = {}, {}
+    for d, j in L.experts():
+        rows = L.span(d, j)
+        _, _, want[d, j], off[d, j] = gated64(dequantised(x[d, rows], xs[d, rows]), w64[d * L.el + j], act, sums(hidden))
+    check_blocks(L, h, hs, want, off, "h")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("counts,in_,out", E4M3_SHAPES + [([[300, 4]], 128, 8), ([[40]], 384, 392), ([[5]], 4096, 2056)])
+def test_product_e4m3(counts, in_, out):
+    L = Layer(counts, 256)
+    (x, xs), (w, ws, w64) = e4m3_rows(L, in_), e4m3_weights(L, out, in_)
+    y = L.unwritten(out)
+    flmoe.fl_moe_expert_product_e4m3(*L.at, in_, out, x.view(torch.uint8), xs, w, ws, y)
+    want, tol = {}, {}
+    for d, j in L.experts():
+        rows = L.span(d, j)
+        x64, we = dequantised(x[d, rows], xs[d, rows]), w64[d * L.el + j]
+        want[d, j] = x64 @ we.T
+        tol[d, j] = want[d, j].abs() * BF16 + (1 + BF16) * sums(in_) * U * (x64.abs() @ we.abs().T) + TINY
+    L.check_rows(y, want, tol, "y")
+
+
+@pytest.mark.gpu
+def test_gradients_against_differences():
+    """The sum of h dh along a direction, by the formula in 64 bits at two points, and by the kernels' gradients: off by
+    what their entries may be off.  dpre is off by two roundings to bf16 (pre, dpre) and dx, dw by one more."""
+    counts, hidden, inter = [[5, 33], [0, 70]], 136, 72
+    for act in (0, 1):
+        L = Layer(counts, hidden, seed=3)
+        x, w, dh = L.rows(hidden), L.weights(2 * inter, hidden), L.rows(inter)
+        h, pre, dpre, dx = L.unwritten(inter), L.unwritten(2 * inter), L.unwritten(2 * inter), L.unwritten(hidden)
+        dw = torch.full_like(w, 77)
+        flmoe.fl_moe_expert_gated(*L.at, inter, act, x, w, h, pre)
+        flmoe.fl_moe_expert_gated_backward(*L.at, inter, act, x, w, pre, None, dh, dpre, dx, dw)
+        for d, j in L.experts():
+            rows, e = L.span(d, j), d * L.el + j
+            xe, we, up = x[d, rows].double(), w[e].double(), dh[d, rows].double()
+
+            def loss(a, b):
+                p = a @ b.T
+                return (act64(p[:, :inter], act)[0] * p[:, inter:] * up).sum()
+            p, dp, _, _ = gated64(xe, we, act)
+            g, u = p[:, :inter], p[:, inter:]
+            a, slope, _ = act64(g, act)
+            err = dp + p.abs() * BF16                       # of the kept pre-activations; no second derivative exceeds 1.6
+            eg, eu = err[:, :inter], err[:, inter:]
+            grad = torch.cat((up * u * slope, up * a), 1)
+            off = torch.cat((up.abs() * (eu * SLOPE + (u.abs() + eu) * 1.6 * eg), up.abs() * SLOPE * eg), 1) + grad.abs() * BF16 * 1.1
+            for got, point, error in ((dx[d, rows], 0, off @ we.abs()), (dw[e], 1, off.T @ xe.abs())):
+                v = torch.randn(got.shape, generator=L.g, device="cuda", dtype=torch.float64)
+                at = [xe, we]
+                lo, hi = list(at), list(at)
+                step = 1e-5
+                lo[point], hi[point] = at[point] - step * v, at[point] + step * v
+                difference = (loss(*hi) - loss(*lo)) / (2 * step)
+                bound = (v.abs() * (error * 1.1 + got.double().abs() * BF16 * 1.1)).sum() + 1e-6
+                assert abs(float((got.double() * v).sum() - difference)) <= float(bound), (act, e, point)
+
+
+@pytest.mark.gpu
+def test_calls_for_part_of_the_ranks_leave_the_others():
+    counts, hidden, inter = [[40, 3], [7, 300], [0, 20], [1, 1]], 256, 128
+    L = Layer(counts, hidden)
+    x, w, dh = L.rows(hidden), L.weights(2 * inter, hidden), L.rows(inter)
+
+    def run(ranges):
+        h, pre, dpre, dx = L.unwritten(inter), L.unwritten(2 * inter), L.unwritten(2 * inter), L.unwritten(hidden)
+        dw = torch.full_like(w, 77)
+        for begin, count in ranges:
+            at = (L.cfg, begin, count, L.expert_off, L.loads)
+            flmoe.fl_moe_expert_gated(*at, inter, 0, x, w, h, pre)
+            flmoe.fl_moe_expert_gated_backward(*at, inter, 0, x, w, pre, None, dh, dpre, dx, dw)
+        return h, pre, dpre, dx, dw
+    whole, parts, some = run([(0, 4)]), run([(2, 2), (0, 1), (1, 1)]), run([(1, 2)])
+    for a, b, c in zip(whole, parts, some):
+        assert torch.equal(a, b)
+        per = c.shape[0] // 4
+        assert torch.equal(c[per:3 * per], a[per:3 * per])
+        for left in (c[:per], c[3 * per:]):
+            assert bool((left == 77).all())
+
+
+@pytest.mark.gpu
+def test_rows_far_behind_the_start():
+    """Rows whose offset passes 32 bits, in elements, in the last rows of a rank's capacity."""
+    hidden, inter, cap = 32768, 128, 70000
+    L = Layer([[5], [37]], hidden, cap=cap, lead=0)
+    L.off = [[0, 5], [cap - 37, cap]]
+    L.expert_off.copy_(torch.tensor(L.off))
+    assert (2 * cap - 37) * hidden > 1 << 32
+    x = torch.zeros((2, cap, hidden), dtype=torch.bfloat16, device="cuda")
+    for d in (0, 1):
+        x[d, L.span(d, 0)] = L.randn(L.counts[d][0], hidden)
+    w = L.weights(2 * inter, hidden)
+    dy, h, dx = torch.zeros((2, cap, inter), dtype=torch.bfloat16, device="cuda"), torch.zeros((2, cap, inter), dtype=torch.bfloat16, device="cuda"), \
+        torch.zeros_like(x)
+    v, dv = L.weights(inter, hidden), torch.empty((2, inter, hidden), dtype=torch.bfloat16, device="cuda")
+    flmoe.fl_moe_expert_gated(*L.at, inter, 0, x, w, h)
+    for d in (0, 1):
+        rows = L.span(d, 0)
+        dy[d, rows] = L.randn(L.counts[d][0], inter)
+        _, _, want, off = gated64(x[d, rows].double(), w[d].double(), 0)
+        check(h[d, rows], want, want.abs() * BF16 + (1 + BF16) * off + TINY, "h")
+    flmoe.fl_moe_expert_product_backward(*L.at, hidden, inter, x, v, dy, dx, dv)
+    for d in (0, 1):
+        rows = L.span(d, 0)
+        de, ve, xe = dy[d, rows].double(), v[d].double(), x[d, rows].double()
+        check(dx[d, rows], de @ ve, (de @ ve).abs() * BF16 + (1 + BF16) * inter * U * (de.abs() @ ve.abs()) + TINY, "dx")
+        check(dv[d], de.T @ xe, (de.T @ xe).abs() * BF16 + (1 + BF16) * 37 * U * (de.abs().T @ xe.abs()) + TINY, "dw")
+
+
+@pytest.mark.gpu
+def test_tables_that_claim_too_much_stay_inside_the_capacity():
+    """What a skipped step leaves in the tables: results are of no use, other memory is not touched."""
+    hidden, inter = 256, 128
+    L = Layer([[4, 4], [4, 4]], hidden, cap=16)
+    x, w = torch.zeros((2, 16, hidden), dtype=torch.bfloat16, device="cuda"), L.weights(2 * inter, hidden)
+    h = torch.full((2 * 16 + 8, inter), 77, dtype=torch.bfloat16, device="cuda")
+    for off, loads in (([[0, 8, 16], [0, 8, 16]], [[4, 9], [100, 1 << 30]]), ([[-5, 16, 17], [1 << 30, -1, 3]], [[3, 3], [7, 7]]),
+                       ([[0, 15, 16], [2, 3, 4]], [[-1, 5], [0x7fffffff, -0x80000000]])):
+        flmoe.fl_moe_expert_gated(L.cfg, 0, 2, torch.tensor(off, dtype=torch.int32, device="cuda"),
+                                  torch.tensor(loads, dtype=torch.int32, device="cuda"), inter, 0, x, w, h)
+        torch.cuda.synchronize()
+        assert bool((h[32:] == 77).all())
+
+
+@pytest.mark.gpu
+def test_infinities_and_nan_stay_in_their_rows():
+    """A row that holds them answers with them; its neighbours, and in the weight gradient its neighbours' columns, do not."""
+    counts, hidden, inter = [[20, 3]], 264, 136
+    L = Layer(counts, hidden)
+    x, w = L.rows(hidden), L.weights(2 * inter, hidden)
+    h, clean = L.unwritten(inter), L.unwritten(inter)
+    flmoe.fl_moe_expert_gated(*L.at, inter, 0, x, w, clean)
+    x[0, 4, 263], x[0, 19, 0] = math.nan, math.inf
+    flmoe.fl_moe_expert_gated(*L.at, inter, 0, x, w, h)
+    fine = [r for r in range(23) if r not in (4, 19)]
+    assert torch.equal(h[0, fine], clean[0, fine])
+    assert bool(h[0, 4].isnan().all()) and not bool(h[0, 19].isfinite().any())
+    dy, dw, before = L.rows(inter), torch.full((2, inter, hidden), 77, dtype=torch.bfloat16, device="cuda"), torch.empty((2, inter, hidden), dtype=torch.bfloat16, device="cuda")
+    flmoe.fl_moe_expert_product_backward(*L.at, hidden, inter, L.rows(hidden), None, dy, None, before)
+    flmoe.fl_moe_expert_product_backward(*L.at, hidden, inter, x, None, dy, None, dw)
+    assert bool(dw[0, :, 263].isnan().all()) and not bool(dw[0, :, 0].isfinite().any())
+    assert bool(dw[0, :, 1:263].isfinite().all()) and bool(dw[1].isfinite().all())
+
+
+@pytest.mark.gpu
+def test_blocks_with_infinities_and_nan():
+    """e4m3 blocks of pre-activations: a NaN is skipped by the maximum, an Inf makes the scale infinite."""
+    hidden = inter = 128
+    L = Layer([[4]], hidden)
+    x = torch.zeros((1, L.cap, hidden), dtype=torch.bfloat16, device="cuda")
+    w = torch.zeros((1, 2 * inter, hidden), dtype=torch.bfloat16, device="cuda")
+    w[0, :inter] = torch.eye(128, device="cuda")            # gates are the row itself
+    x[0, 0, :3] = torch.tensor([448.0, -1.0, 0.5], device="cuda")
+    x[0, 1, 0], x[0, 1, 1] = 896.0, -2.0
+    h, pre, scales = L.unwritten(inter), L.unwritten(2 * inter, torch.uint8), L.unwritten(2, torch.float32)
+    flmoe.fl_moe_expert_gated(*L.at, inter, 0, x, w, h, pre, scales)
+    assert scales[0, :4, 0].tolist() == [1.0, 2.0, 1.0, 1.0] and scales[0, :4, 1].tolist() == [1.0] * 4
+    assert pre[0, 0, :4].tolist() == [0x7e, 0xb8, 0x30, 0] and pre[0, 1, :3].tolist() == [0x7e, 0xb8, 0]
+    # gates of inf and -inf among finite ones: 0 * inf elsewhere in the row is NaN
+    x.zero_()
+    x[0, 0, 5], x[0, 1, 5] = math.inf, -math.inf
+    flmoe.fl_moe_expert_gated(*L.at, inter, 0, x, w, h, pre, scales)
+    assert math.isinf(float(scales[0, 0, 0])) and math.isinf(float(scales[0, 1, 0]))
+    assert int(pre[0, 0, 5]) == 0x7f and int(pre[0, 1, 5]) == 0xff
+    assert bool(((pre[0, :2] & 0x7f) == 0x7f)[:, :128].all())
+
+
+@pytest.mark.gpu
+def test_runs_agree_bit_for_bit_also_on_another_stream_and_in_a_graph():
+    counts, hidden, inter = [[40, 300], [513, 0]], 1024, 256
+    L = Layer(counts, hidden)
+    x, w, dh = L.rows(hidden), L.weights(2 * inter, hidden), L.rows(inter)
+    (x8, xs), (w8, ws, _) = e4m3_rows(L, hidden), e4m3_weights(L, 2 * inter, hidden)
+    v8, vs, _ = e4m3_weights(L, hidden, inter)
+
+    def buffers():
+        return [L.unwritten(inter), L.unwritten(2 * inter), L.unwritten(2 * inter), L.unwritten(hidden), torch.full_like(w, 77),
+                L.unwritten(inter, torch.uint8), L.unwritten(inter // 128, torch.float32), L.unwritten(hidden)]
+
+    def run(b, stream=None):
+        h, pre, dpre, dx, dw, h8, hs, y = b
+        flmoe.fl_moe_expert_gated(*L.at, inter, 0, x, w, h, pre, stream=stream)
+        flmoe.fl_moe_expert_gated_backward(*L.at, inter, 0, x, w, pre, None, dh, dpre, dx, dw, stream=stream)
+        flmoe.fl_moe_expert_gated_e4m3(*L.at, inter, 1, x8, xs, w8, ws, h8, hs, stream=stream)
+        flmoe.fl_moe_expert_product_e4m3(*L.at, inter, hidden, h8, hs, v8, vs, y, stream=stream)
+    first, second, third = buffers(), buffers(), buffers()
+    run(first)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    run(second, side)
+    torch.cuda.current_stream().wait_stream(side)
+    for a, b in zip(first, second):
+        assert torch.equal(a, b)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        run(third)
+    for seed in range(3):                            # new inputs in the same buffers, eager work between the replays
+        x.copy_(L.rows(hidden))
+        x8.view(torch.uint8)[L.used] = x8.view(torch.uint8)[L.used].flip(0)
+        for t in third:
+            t.fill_(77)
+        graph.replay()
+        torch.cuda.synchronize()
+        run(first)
+        for a, b in zip(first, third):
+            assert torch.equal(a, b), seed
+
+
+@pytest.mark.gpu
+def test_the_binding_refuses_wrong_tensors():
+    L = Layer([[4, 4]], 256)
+    x, w, h = L.rows(256), L.weights(256, 256), L.unwritten(128)
+    ok = (*L.at, 128, 0, x, w, h)
+    flmoe.fl_moe_expert_gated(*ok)
+    for place, bad in ((7, x.float()), (7, x[:, :-1]), (7, x.transpose(1, 2)), (8, w[:1]), (8, w.cpu()), (9, h[..., ::2]), (9, None),
+                       (3, L.expert_off.long()), (4, L.loads[:, :1])):
+        args = list(ok)
+        args[place] = bad
+        with pytest.raises(flmoe.FlMoeError) as e:
+            flmoe.fl_moe_expert_gated(*args)
+        assert e.value.code == INVALID, place
