@@ -53,6 +53,12 @@ __device__ inline Rows rows_of(const Groups &G, int e) {
     return {n ? (long long)d * G.cap + off : 0, (int)n};
 }
 
+// A value that is the same in all lanes, in scalar registers.
+__device__ inline long long same_in_wave(long long v) {
+    const unsigned lo = __builtin_amdgcn_readfirstlane((int)(unsigned)v), hi = __builtin_amdgcn_readfirstlane((int)(v >> 32));
+    return (long long)((unsigned long long)hi << 32 | lo);
+}
+
 // ---------------------------------------------------------------- numbers
 __device__ inline float from_bf16(unsigned bits) { return __uint_as_float(bits << 16); }
 __device__ inline unsigned to_bf16(float f) {
@@ -99,21 +105,34 @@ __device__ inline unsigned e4m3_codes(const float *v, float scale) {
 }
 
 // ---------------------------------------------------------------- memory
-// A lane's 16 (or 4) bytes straight into LDS, at the wave's base plus 16 (4) times the lane; offsets of kNowhere read as zero.
-// Only addresses inside the tensor or kNowhere are ever passed, the limit is the largest that an offset can be checked against.
-constexpr unsigned kNowhere = 0x80000000u;
+// A lane's 16 (or 4) bytes straight into LDS, at the wave's place there plus 16 (4) times the lane.  Offsets of kNowhere
+// read as zero; only offsets inside the tensor or kNowhere are ever passed, the limit is the largest there is.  Written
+// out because the compiler, which knows that these loads write LDS, lets every read of LDS behind them wait for them:
+// here the waits are the ones below, once per step.  Nothing is returned, so no register is written behind its back.
+// (One wait state lies between a write of m0 and a load that goes by it.)
 #define FLMOE_LDS __attribute__((address_space(3)))
-__device__ inline __amdgpu_buffer_rsrc_t window(const char *base) {
-    return __builtin_amdgcn_make_buffer_rsrc((void *)base, 0, 0x7FFFFFFF, 0x00020000);
+constexpr unsigned kNowhere = 0x80000000u;
+struct Window {
+    v4u rsrc;
+    __device__ explicit Window(const char *base) {
+        const unsigned long long at = (unsigned long long)base;
+        rsrc = v4u{(unsigned)at, (unsigned)(at >> 32) & 0xffffu, 0x7FFFFFFFu, 0x00020000u};
+    }
+};
+__device__ inline unsigned lds_address(const char *lds) { return (unsigned)(uintptr_t)(FLMOE_LDS const char *)lds; }
+__device__ inline void to_lds_16(const Window &w, unsigned offset, unsigned shift, unsigned lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                 ::"s"(lds), "v"(offset), "s"(w.rsrc), "s"(shift) : "memory");
 }
-__device__ inline void to_lds_16(const char *base, unsigned offset, char *lds) {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(window(base), (FLMOE_LDS void *)lds, 16, offset, 0, 0, 0);
+__device__ inline void to_lds_4(const Window &w, unsigned offset, unsigned shift, unsigned lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds"
+                 ::"s"(lds), "v"(offset), "s"(w.rsrc), "s"(shift) : "memory");
 }
-__device__ inline void to_lds_4(const char *base, unsigned offset, char *lds) {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(window(base), (FLMOE_LDS void *)lds, 4, offset, 0, 0, 0);
+// Every load of this wave but the last KEEP is done, and so is every wave's, and its reads of LDS, behind the barrier.
+template <int KEEP>
+__device__ inline void loads_done_and_barrier() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(KEEP) : "memory");
 }
-// Every load and store of this wave is done.
-__device__ inline void loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 // ---------------------------------------------------------------- the tiles' geometry
 constexpr int kThreads = 512, kWaves = kThreads / kWave;
@@ -241,26 +260,26 @@ struct Tile {
             off_s = (unsigned)r * per_row * 4;
         }
 
+        const unsigned lds0 = lds_address(lds);
         auto stage = [&](int step, int s) {
-            char *at = lds + s * kStage;
-            const bool there_a = kTransA || step * kStep + chunk * 16 < k * size;
+            const unsigned at = lds0 + s * kStage;
+            const int row = wave * 2 + (lane >> 5);                    // transposed operands: of the first load
+            const bool there = step * kStep + chunk * 16 < k * size;   // the others
+            const Window wa(kTransA ? a0 + (size_t)step * 64 * P.a_ld : a0), wa1(a1);
+            const Window wb(kTransB ? b0 + (size_t)step * 64 * P.b_ld : b0);
 #pragma unroll
             for (int j = 0; j < kLoadsA; ++j) {
-                unsigned off = off_a[j];
-                if (kTransA) off = step * 64 + (j * kWaves + wave) * 2 + (lane >> 5) < k ? off : kNowhere;
-                else off = there_a ? off : kNowhere;
-                const char *base = GATED && j >= kLoadsA / 2 ? a1 : a0;
-                to_lds_16(base + (kTransA ? (size_t)step * 64 * P.a_ld : (size_t)step * kStep), off, at + (j * kWaves + wave) * 1024);
+                const bool valid = kTransA ? step * 64 + j * kWaves * 2 + row < k : there;
+                to_lds_16(GATED && j >= kLoadsA / 2 ? wa1 : wa, valid ? off_a[j] : kNowhere, kTransA ? 0 : step * kStep,
+                          at + (j * kWaves + wave) * 1024);
             }
 #pragma unroll
             for (int j = 0; j < kLoadsB; ++j) {
-                unsigned off = off_b[j];
-                if (kTransB) off = step * 64 + (j * kWaves + wave) * 2 + (lane >> 5) < k ? off : kNowhere;
-                else off = step * kStep + chunk * 16 < k * size ? off : kNowhere;
-                to_lds_16(b0 + (kTransB ? (size_t)step * 64 * P.b_ld : (size_t)step * kStep), off, at + kBytesA + (j * kWaves + wave) * 1024);
+                const bool valid = kTransB ? step * 64 + j * kWaves * 2 + row < k : there;
+                to_lds_16(wb, valid ? off_b[j] : kNowhere, kTransB ? 0 : step * kStep, at + kBytesA + (j * kWaves + wave) * 1024);
             }
             if (E4M3 && wave < ROWS / kWave)
-                to_lds_4((const char *)(sb + step), off_s, at + kBytesA + kBytesB + wave * kWave * 4);
+                to_lds_4(Window((const char *)sb), off_s, step * 4, at + kBytesA + kBytesB + wave * kWave * 4);
         };
 
         Acc acc[kFragsF][kFragsR];
@@ -329,12 +348,12 @@ struct Tile {
             }
         };
 
+        __syncthreads();                           // the tile before is done with its LDS
+        if (steps) stage(0, 0);
         for (int step = 0; step < steps; ++step) {
-            __syncthreads();                       // the operands of the step before (or the tile before) are done with
-            stage(step, 0);
-            loads_done();
-            __syncthreads();
-            multiply(step, 0);
+            loads_done_and_barrier<0>();           // this step's operands are there, those of the step before are done with
+            if (step + 1 < steps) stage(step + 1, (step + 1) % STAGES);
+            multiply(step, step % STAGES);
         }
 
         // ---- the tile's output, 128 features at a time through LDS, so that rows are written in whole lines
@@ -475,11 +494,11 @@ __global__ __launch_bounds__(kThreads) void expert_tiles_kernel(Groups G, Produc
         const int group = index / (kRowGroup * columns), left = n_tiles - group * kRowGroup;
         const int in_group = left < kRowGroup ? left : kRowGroup, within = index - group * kRowGroup * columns;
         const int column = within / in_group, row = group * kRowGroup + within - column * in_group;
-        const int e = G.first + lo;
-        const Rows rows = rows_of(G, e);
+        const int e = G.first + __builtin_amdgcn_readfirstlane(lo);
+        const Rows found = rows_of(G, e), rows = {same_in_wave(found.first), __builtin_amdgcn_readfirstlane(found.n)};
         // (tables that claim more rows than there can be may have wrapped the sums)
         if ((unsigned)column >= (unsigned)columns || row < 0 || (long long)row * ROWS >= (FORM == kWeightGradient ? P.other : rows.n)) continue;
-        T::run(P, lds, e, rows, column * T::kOutput, row * ROWS);
+        T::run(P, lds, e, rows, __builtin_amdgcn_readfirstlane(column) * T::kOutput, __builtin_amdgcn_readfirstlane(row) * ROWS);
     }
 }
 
