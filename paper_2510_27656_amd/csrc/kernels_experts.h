@@ -156,12 +156,13 @@ struct Product {
     int act;
 };
 
-// Place of a 16-byte chunk in a staged operand.
-// Contiguous along the contraction: rows of 128 bytes, chunk c of row r at c ^ (r & 7): eight rows read at one chunk
-// fall into eight different sixteenths of the banks.
-// Contiguous along the features: 64 contraction rows of 512 bytes; the transposing reads take 32 bytes of 16 rows
-// (k .. k+3 of four groups eight apart), which this spreads over the whole row.
-__device__ inline int spread(int row) { return ((row & 3) | (row >> 3 & 3) << 2) << 1; }
+// Place of a 16-byte chunk in a staged operand, so that the lanes that are served together fall into different banks
+// (64 of 4 bytes; sixteen lanes of a 16-byte read, 32 of an 8-byte one).
+// Contiguous along the contraction: rows of 128 bytes, chunk c of row r at c ^ (r >> 1 & 7): two rows fill the banks once.
+// Contiguous along the features: 64 contraction rows of 512 bytes, chunk c of row r at c ^ (r & 3) << 2: the transposing
+// reads take 64 bytes each of four rows at once.
+__device__ inline int swizzle(int row) { return row >> 1 & 7; }
+__device__ inline int spread(int row) { return (row & 3) << 2; }
 
 // Four rows of the contraction for one feature per lane: lanes 16 i .. 16 i + 15 give the places of four rows by four
 // chunks of 8 bytes, and lane j of them receives column j.
@@ -205,7 +206,7 @@ struct Tile {
         // where this lane's chunks come from: offsets inside the operands, places that must not be past the end
         const char *a0, *a1, *b0;                                      // a1: ups of a gated tile
         unsigned off_a[kLoadsA], off_b[kLoadsB];
-        const int chunk = (lane & 7) ^ (lane >> 3);
+        const int chunk = (lane & 7) ^ swizzle(wave * 8 + (lane >> 3));       // (eight waves on it is the same)
         if (kTransA) {
             a0 = FORM == kWeightGradient ? P.a + (size_t)rows.first * P.a_ld : P.a + (size_t)e * P.a_expert;
             a1 = a0;
@@ -298,8 +299,8 @@ struct Tile {
                 v8i fb[kFragsR];
                 float scale[kFragsR];
                 auto frag = [&](const char *T, int row) {
-                    const v4i lo = *(const v4i *)(T + row * kStep + (((lane >> 4) ^ (row & 7)) << 4));
-                    const v4i hi = *(const v4i *)(T + row * kStep + ((((lane >> 4) + 4) ^ (row & 7)) << 4));
+                    const v4i lo = *(const v4i *)(T + row * kStep + (((lane >> 4) ^ swizzle(row)) << 4));
+                    const v4i hi = *(const v4i *)(T + row * kStep + ((((lane >> 4) + 4) ^ swizzle(row)) << 4));
                     return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
                 };
 #pragma unroll
@@ -330,7 +331,7 @@ struct Tile {
                         return __builtin_bit_cast(v8bf, both);
                     }
                     const int row = first + (lane & 31);
-                    return *(const v8bf *)(T + row * kStep + (((part * 2 + (lane >> 5)) ^ (row & 7)) << 4));
+                    return *(const v8bf *)(T + row * kStep + (((part * 2 + (lane >> 5)) ^ swizzle(row)) << 4));
                 };
 #pragma unroll
                 for (int part = 0; part < 4; ++part) {
