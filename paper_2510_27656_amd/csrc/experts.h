@@ -61,7 +61,7 @@ inline int launched() { return hipGetLastError() == hipSuccess ? FL_OK : FL_ERR_
 template <int FORM, bool E4M3, bool GATED>
 int launch_tiles(const Groups &G, const Product &P, hipStream_t st) {
     const int grid = std::max(1, compute_units() / kXcds) * kXcds;
-    expert_tiles_kernel<FORM, E4M3, GATED, 256, 2><<<dim3(grid), dim3(kThreads), 0, st>>>(G, P);
+    expert_tiles_kernel<FORM, E4M3, GATED, 256><<<dim3(grid), dim3(kThreads), 0, st>>>(G, P);
     return launched();
 }
 

@@ -134,11 +134,21 @@ __device__ inline void loads_done_and_barrier() {
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(KEEP) : "memory");
 }
 
-// ---------------------------------------------------------------- the tiles' geometry
+// ---------------------------------------------------------------- the tiles
+// 256 features by 256 rows, eight waves, two on each SIMD.  A step multiplies 128 bytes of the contraction (64 bf16, 128
+// e4m3).  Both operands of a step come in two units of 16 KB (A0, A1: 128 features each, of a gated tile the gates and their
+// ups; B0, B1: 128 rows each), and each wave owns 64 of the features and 32 of the rows of every unit.  A step has four
+// phases, in each of which a wave multiplies what it holds in registers while it reads the next phase's share from LDS:
+//   phase 1: A0 B0, reads B1     phase 2: A0 B1, reads A1 over A0, fragment by fragment as they are used up
+//   phase 3: A1 B1, reads B0 of the next step     phase 4: A1 B0, reads A0 of the next step over A1
+// So a unit's LDS is free again one phase after it was first touched, and with two places for each unit the loads that
+// fill it have almost two steps to arrive: 128 KB are on their way to a compute unit nearly all the time.  Between
+// phases: this wave's reads are done, its oldest loads have arrived, barrier.
 constexpr int kThreads = 512, kWaves = kThreads / kWave;
-constexpr int kStep = 128;                     // bytes of the contraction per step: 64 bf16, 128 e4m3 (one block of scales)
-constexpr int kFeatures = 256;                 // features of a tile; gated: 128 gates and the 128 ups that belong to them
-constexpr int kHalf = 128;                     // features that are written out together
+constexpr int kStep = 128;                     // bytes of the contraction per step
+constexpr int kHalf = 128;                     // features, or rows, of a unit
+constexpr int kUnit = kHalf * kStep;
+constexpr int kFeatures = 2 * kHalf;
 constexpr int kEmitPitch = kHalf + 4;          // floats from row to row of the tile's output in LDS
 
 enum Form { kForward, kRowGradient, kWeightGradient };
@@ -156,227 +166,283 @@ struct Product {
     int act;
 };
 
-// Place of a 16-byte chunk in a staged operand, so that the lanes that are served together fall into different banks
-// (64 of 4 bytes; sixteen lanes of a 16-byte read, 32 of an 8-byte one).
+// Place of a 16-byte chunk in a unit, so that the lanes that are served together fall into different banks (64 of 4
+// bytes; sixteen lanes of a 16-byte read, 32 of an 8-byte one).
 // Contiguous along the contraction: rows of 128 bytes, chunk c of row r at c ^ (r >> 1 & 7): two rows fill the banks once.
-// Contiguous along the features: 64 contraction rows of 512 bytes, chunk c of row r at c ^ (r & 3) << 2: the transposing
+// Contiguous along the features: 64 contraction rows of 256 bytes, chunk c of row r at c ^ (r & 3) << 2: the transposing
 // reads take 64 bytes each of four rows at once.
 __device__ inline int swizzle(int row) { return row >> 1 & 7; }
 __device__ inline int spread(int row) { return (row & 3) << 2; }
 
-// Four rows of the contraction for one feature per lane: lanes 16 i .. 16 i + 15 give the places of four rows by four
-// chunks of 8 bytes, and lane j of them receives column j.
-__device__ inline v4s read_transposed(const char *lds, int row, int feature) {
-    const int l = threadIdx.x & 15;
-    const int r = row + (l >> 2), c = (feature >> 3) + (l >> 1 & 1);
-    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((FLMOE_LDS v4s *)(lds + r * 512 + ((c ^ spread(r)) << 4) + (l & 1) * 8));
-}
-
-template <int FORM, bool E4M3, bool GATED, int ROWS, int STAGES>
+template <int FORM, bool E4M3, bool GATED, int ROWS>
 struct Tile {
     static constexpr bool kTransA = FORM != kForward, kTransB = FORM == kWeightGradient;
-    static constexpr int kWavesF = ROWS == 256 ? 2 : 4, kWavesR = kWaves / kWavesF;
     static constexpr int kSide = E4M3 ? 16 : 32;                       // of a matrix instruction's output
-    static constexpr int kFragsF = kFeatures / kWavesF / kSide, kFragsR = ROWS / kWavesR / kSide;
-    static constexpr int kBytesA = kFeatures * kStep, kBytesB = ROWS * kStep, kBytesS = E4M3 ? ROWS * 4 : 0;
-    static constexpr int kStage = kBytesA + kBytesB + kBytesS;
+    static constexpr int kParts = E4M3 ? 1 : 4;                        // matrix instructions along a step
+    static constexpr int kFragsF = 64 / kSide, kFragsR = 32 / kSide;   // of a wave in a unit
+    static constexpr int kHalves = ROWS / kHalf;
+    static constexpr int kScales = E4M3 ? kWaves * kWave * 4 : 0;      // of a step: 64 rows' for each wave
+    static constexpr int kScaleSlots = 4;
+    static constexpr int kRing = 2 * (2 + kHalves) * kUnit;            // [two][A0, A1, B0, B1]
     static constexpr int kEmit = ROWS * kEmitPitch * 4;
-    static constexpr int kLds = STAGES * kStage > kEmit ? STAGES * kStage : kEmit;
+    static constexpr int kLds = (kRing > kEmit ? kRing : kEmit) + kScaleSlots * kScales;
     static constexpr int kOutput = GATED ? kHalf : kFeatures;          // output features of a tile
-    static constexpr int kLoadsA = kBytesA / 1024 / kWaves, kLoadsB = kBytesB / 1024 / kWaves;
-    static_assert(!kTransB || ROWS == 256, "transposed operands are 256 wide");
     using Acc = typename std::conditional<E4M3, v4f, v16f>::type;
+    using Frag = typename std::conditional<E4M3, v8i, v8bf>::type;
     static constexpr int kAccs = E4M3 ? 4 : 16;
+    enum Unit { A0, A1, B0, B1 };
 
-    // First feature, of the staged 256, of fragment i of this wave.
-    __device__ static int frag_feature(int wf, int i) {
-        if (!GATED) return (wf * kFragsF + i) * kSide;
-        return (i < kFragsF / 2 ? 0 : kHalf) + (wf * (kFragsF / 2) + i % (kFragsF / 2)) * kSide;
-    }
-
-    // e: expert; first, n: its rows; f0: first output feature; r0: first row (weight gradient: first column of b).
+    // e: expert; rows: its rows; f0: first output feature; r0: first row (weight gradient: first column of b).
     __device__ static void run(const Product &P, char *lds, int e, const Rows &rows, int f0, int r0) {
         const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-        const int wf = wave % kWavesF, wr = wave / kWavesF;
+        const int wf = wave & 1, wr = wave >> 1;
         const int size = E4M3 ? 1 : 2;
         const int k = FORM == kWeightGradient ? rows.n : P.k;          // contraction
         const int n_b = FORM == kWeightGradient ? P.other : rows.n;    // rows of operand b
-        const int steps = (k * (long long)size + kStep - 1) / kStep;
+        const int steps = (int)(((long long)k * size + kStep - 1) / kStep);
 
-        // where this lane's chunks come from: offsets inside the operands, places that must not be past the end
+        // Where this lane's chunks come from.  Features and rows past the end are replaced by ones that are there (what
+        // is computed from them is not written), the contraction's by zeros.
+        unsigned off[2][4];                        // [operand][two loads of each unit]
+        int steps_here[2];                         // steps in which this lane's chunk of a load is there (transposed: of both)
+        const int chunk = (lane & 7) ^ swizzle(wave * 8 + (lane >> 3));           // as lies, contiguous along the contraction
+        const int column = ((lane & 15) ^ spread(lane >> 4)) * 8, depth = wave * 4 + (lane >> 4);   // transposed
+#pragma unroll
+        for (int o = 0; o < 2; ++o) {
+            const bool trans = o ? kTransB : kTransA;
+            const int ld = o ? P.b_ld : P.a_ld, end = o ? n_b - r0 : P.features - f0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (trans) {
+                    int f = (j >> 1) * kHalf + column;
+                    if (f >= end) f = 0;
+                    off[o][j] = (unsigned)(depth + (j & 1) * 32) * ld + f * 2;
+                } else {
+                    int r = (j * kWaves + wave) * 8 + (lane >> 3);
+                    if (!o && GATED) r &= kHalf - 1;
+                    if (r >= end) r = 0;
+                    off[o][j] = (unsigned)r * ld + chunk * 16;
+                }
+            }
+            steps_here[o] = trans ? (k - depth + 63) / 64 : (k * size - chunk * 16 + kStep - 1) / kStep;
+        }
         const char *a0, *a1, *b0;                                      // a1: ups of a gated tile
-        unsigned off_a[kLoadsA], off_b[kLoadsB];
-        const int chunk = (lane & 7) ^ swizzle(wave * 8 + (lane >> 3));       // (eight waves on it is the same)
-        if (kTransA) {
-            a0 = FORM == kWeightGradient ? P.a + (size_t)rows.first * P.a_ld : P.a + (size_t)e * P.a_expert;
-            a1 = a0;
-#pragma unroll
-            for (int j = 0; j < kLoadsA; ++j) {
-                const int r = (j * kWaves + wave) * 2 + (lane >> 5);
-                int f = f0 + ((lane & 31) ^ spread(r)) * 8;
-                if (f >= P.features) f = 0;
-                off_a[j] = (unsigned)r * P.a_ld + f * 2;
-            }
-        } else {
-            const char *base = P.a + (size_t)e * P.a_expert;
-            a0 = base + (size_t)f0 * P.a_ld;
-            a1 = GATED ? a0 + (size_t)P.features * P.a_ld : a0;
-#pragma unroll
-            for (int j = 0; j < kLoadsA; ++j) {
-                int r = (j * kWaves + wave) * 8 + (lane >> 3);
-                if (GATED) r &= kHalf - 1;
-                if (f0 + r >= P.features) r = 0;
-                off_a[j] = (unsigned)r * P.a_ld + chunk * 16;
-            }
-        }
-        if (kTransB) {
-            b0 = P.b + (size_t)rows.first * P.b_ld;
-#pragma unroll
-            for (int j = 0; j < kLoadsB; ++j) {
-                const int r = (j * kWaves + wave) * 2 + (lane >> 5);
-                int f = r0 + ((lane & 31) ^ spread(r)) * 8;
-                if (f >= n_b) f = 0;
-                off_b[j] = (unsigned)r * P.b_ld + f * 2;
-            }
-        } else {
-            b0 = P.b + (size_t)(rows.first + r0) * P.b_ld;
-#pragma unroll
-            for (int j = 0; j < kLoadsB; ++j) {
-                int r = (j * kWaves + wave) * 8 + (lane >> 3);
-                if (r0 + r >= n_b) r = 0;
-                off_b[j] = (unsigned)r * P.b_ld + chunk * 16;
-            }
-        }
-        const float *sa = nullptr, *sa1 = nullptr, *sb = nullptr;
+        if (FORM == kWeightGradient) a0 = P.a + (size_t)rows.first * P.a_ld + f0 * 2;
+        else a0 = P.a + (size_t)e * P.a_expert + (kTransA ? (size_t)f0 * 2 : (size_t)f0 * P.a_ld);
+        a1 = GATED ? a0 + (size_t)P.features * P.a_ld : a0;
+        b0 = kTransB ? P.b + (size_t)rows.first * P.b_ld + r0 * 2 : P.b + (size_t)(rows.first + r0) * P.b_ld;
+        // (weights never change while a kernel runs: scalar loads)
+        typedef const __attribute__((address_space(4))) float *Constant;
+        Constant sa[2] = {nullptr, nullptr};
+        const char *sb = nullptr;
         unsigned off_s = 0;
-        if (E4M3) {                                                    // scales: one of a row and one of 128 features a step
-            const int blocks = (P.features + 127) / 128 * (GATED ? 2 : 1), per_row = P.k / 128;
-            const int first = f0 / 128 + (GATED ? 0 : frag_feature(wf, 0) / 128);
-            const int last = (P.features - 1) / 128;
-            sa = P.a_scales + ((size_t)e * blocks + (first < last ? first : last)) * per_row;
-            sa1 = GATED ? sa + (size_t)(P.features / 128) * per_row : sa;
-            sb = P.b_scales + (size_t)(rows.first + r0) * per_row;
-            int r = wave * kWave + lane;
-            if (r0 + r >= n_b) r = 0;
+        const int per_row = P.k / 128;
+        if (E4M3) {                                                    // scales: of a row and of 128 features, one a step
+            const int blocks = (P.features + 127) / 128;
+            const Constant first = (Constant)(uintptr_t)P.a_scales + (size_t)e * blocks * (GATED ? 2 : 1) * per_row + (size_t)(f0 / 128) * per_row;
+            sa[0] = first;
+            sa[1] = GATED ? first + (size_t)blocks * per_row : f0 / 128 + 1 < blocks ? first + per_row : first;
+            sb = (const char *)(P.b_scales + (size_t)(rows.first + r0) * per_row);
+            int r = (lane >> 5) * kHalf + wr * 32 + (lane & 31);       // lane: B0's rows of this wave, then B1's
+            if (r >= n_b - r0) r = 0;
             off_s = (unsigned)r * per_row * 4;
         }
 
         const unsigned lds0 = lds_address(lds);
-        auto stage = [&](int step, int s) {
-            const unsigned at = lds0 + s * kStage;
-            const int row = wave * 2 + (lane >> 5);                    // transposed operands: of the first load
-            const bool there = step * kStep + chunk * 16 < k * size;   // the others
-            const Window wa(kTransA ? a0 + (size_t)step * 64 * P.a_ld : a0), wa1(a1);
-            const Window wb(kTransB ? b0 + (size_t)step * 64 * P.b_ld : b0);
+        // [slot][A0, A1], then [slot][B0, B1]: what one operand's reads span fits their instructions' offset
+        auto place = [](int unit, int slot) constexpr { return unit < B0 ? (slot * 2 + unit) * kUnit : (4 + slot * kHalves + unit - B0) * kUnit; };
+        constexpr int kScalesAt = kRing > kEmit ? kRing : kEmit;
+        auto scales_at = [&](int step) { return kScalesAt + ((step & (kScaleSlots - 1)) * kWaves + wave) * kWave * 4; };
+        auto load = [&](int unit, int step) {
+            const int o = unit >= B0, u = o ? unit - B0 : unit;
+            const bool trans = o ? kTransB : kTransA;
+            const int ld = o ? P.b_ld : P.a_ld;
+            const char *base = o ? b0 : u ? a1 : a0;
+            const Window from(trans ? base + (size_t)step * 64 * ld : base);
+            const unsigned to = lds0 + place(unit, step & 1) + wave * 1024;
 #pragma unroll
-            for (int j = 0; j < kLoadsA; ++j) {
-                const bool valid = kTransA ? step * 64 + j * kWaves * 2 + row < k : there;
-                to_lds_16(GATED && j >= kLoadsA / 2 ? wa1 : wa, valid ? off_a[j] : kNowhere, kTransA ? 0 : step * kStep,
-                          at + (j * kWaves + wave) * 1024);
+            for (int j = 0; j < 2; ++j) {
+                const bool there = trans && j ? step * 64 + depth + 32 < k : step < steps_here[o];
+                to_lds_16(from, there ? off[o][u * 2 + j] : kNowhere, trans ? 0 : step * kStep, to + j * kWaves * 1024);
             }
-#pragma unroll
-            for (int j = 0; j < kLoadsB; ++j) {
-                const bool valid = kTransB ? step * 64 + j * kWaves * 2 + row < k : there;
-                to_lds_16(wb, valid ? off_b[j] : kNowhere, kTransB ? 0 : step * kStep, at + kBytesA + (j * kWaves + wave) * 1024);
-            }
-            if (E4M3 && wave < ROWS / kWave)
-                to_lds_4(Window((const char *)sb), off_s, step * 4, at + kBytesA + kBytesB + wave * kWave * 4);
+        };
+        auto load_scales = [&](int step) {
+            if (E4M3) to_lds_4(Window(sb), step < steps ? off_s : kNowhere, step * 4, lds0 + scales_at(step));
         };
 
-        Acc acc[kFragsF][kFragsR];
+        // This wave's fragments of a unit.  Their places differ from the first one's by constants and, where the swizzle
+        // reaches into them, by one of a few patterns: those are kept as addresses.
+        //   bf16: 8 values of a row from chunk 2 part + (lane >> 5) on; a pattern for each part
+        //   e4m3: chunks lane >> 4 and that plus 4 (any order of the contraction will do that both operands have)
+        //   transposed: lanes 16 i .. 16 i + 15 give the places of four rows by four pieces of 8 bytes, and lane j of them
+        //   receives column j; a pattern for each fragment
+        constexpr int kPatterns = 4;
+        unsigned at[2][kPatterns];
 #pragma unroll
-        for (int i = 0; i < kFragsF; ++i)
+        for (int o = 0; o < 2; ++o) {
+            const int first = o ? wr * 32 : wf * 64, unit = lds0 + place(o ? B0 : A0, 0);
 #pragma unroll
-            for (int j = 0; j < kFragsR; ++j)
-#pragma unroll
-                for (int t = 0; t < kAccs; ++t) acc[i][j][t] = 0.0f;
-
-        auto multiply = [&](int step, int s) {
-            const char *A = lds + s * kStage, *B = A + kBytesA;
-            if constexpr (E4M3) {
-                const float *S = (const float *)(B + kBytesB);
-                const float wa = sa[step], wa1 = GATED ? sa1[step] : wa;
-                v8i fb[kFragsR];
-                float scale[kFragsR];
-                auto frag = [&](const char *T, int row) {
-                    const v4i lo = *(const v4i *)(T + row * kStep + (((lane >> 4) ^ swizzle(row)) << 4));
-                    const v4i hi = *(const v4i *)(T + row * kStep + ((((lane >> 4) + 4) ^ swizzle(row)) << 4));
-                    return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-                };
-#pragma unroll
-                for (int j = 0; j < kFragsR; ++j) {
-                    const int row = (wr * kFragsR + j) * kSide + (lane & 15);
-                    fb[j] = frag(B, row);
-                    scale[j] = S[row];
+            for (int p = 0; p < kPatterns; ++p) {
+                if (E4M3) {
+                    const int row = lane & 15;
+                    at[o][p] = unit + (first + row) * kStep + (((lane >> 4) + (p & 1) * 4) ^ swizzle(row)) * 16;
+                } else if (o ? kTransB : kTransA) {
+                    const int row = (lane >> 5) * 8 + (lane >> 2 & 3), c = (first + p * kSide + (lane & 16)) / 8 + (lane >> 1 & 1);
+                    at[o][p] = unit + row * 256 + (c ^ spread(row)) * 16 + (lane & 1) * 8;
+                } else {
+                    const int row = lane & 31;
+                    at[o][p] = unit + (first + row) * kStep + ((p * 2 + (lane >> 5)) ^ swizzle(row)) * 16;
                 }
+                asm volatile("" : "+v"(at[o][p]));                     // not to be worked out again at every use
+            }
+        }
+        auto frag = [&](auto unit, auto slot, int i, int part) -> Frag {
+            constexpr int o = unit() >= B0, base = place(unit(), slot()) - place(o ? B0 : A0, 0);
+            if constexpr (E4M3) {
+                const v4i lo = *(FLMOE_LDS const v4i *)(uintptr_t)(at[o][0] + base + i * kSide * kStep);
+                const v4i hi = *(FLMOE_LDS const v4i *)(uintptr_t)(at[o][1] + base + i * kSide * kStep);
+                return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+            } else if constexpr (o ? kTransB : kTransA) {
+                const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((FLMOE_LDS v4s *)(uintptr_t)(at[o][i] + base + part * 4096));
+                const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((FLMOE_LDS v4s *)(uintptr_t)(at[o][i] + base + part * 4096 + 1024));
+                const v8s both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+                return __builtin_bit_cast(v8bf, both);
+            } else {
+                return *(FLMOE_LDS const v8bf *)(uintptr_t)(at[o][part] + base + i * kSide * kStep);
+            }
+        };
+        using U_A0 = std::integral_constant<int, A0>;
+        using U_A1 = std::integral_constant<int, A1>;
+        using U_B0 = std::integral_constant<int, B0>;
+        using U_B1 = std::integral_constant<int, B1>;
+
+        Acc acc[2][kHalves][kFragsF][kFragsR];
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int g = 0; g < kHalves; ++g)
+#pragma unroll
+                for (int i = 0; i < kFragsF; ++i)
+#pragma unroll
+                    for (int j = 0; j < kFragsR; ++j)
+#pragma unroll
+                        for (int t = 0; t < kAccs; ++t) acc[h][g][i][j][t] = 0.0f;
+
+        Frag fa[kFragsF][kParts], fb0[2][kFragsR][kParts], fb1[kFragsR][kParts];
+        float row_scale[2][kFragsR];
+        // multiplies the fragments at hand into quadrant (h, g); next(i, part) follows a fragment's last use
+        auto multiply = [&](auto half_a, auto half_b, const Frag (&b)[kFragsR][kParts], float w, auto next) {
+            constexpr int h = decltype(half_a)::value, g = decltype(half_b)::value;
+#pragma unroll
+            for (int part = 0; part < kParts; ++part)
 #pragma unroll
                 for (int i = 0; i < kFragsF; ++i) {
-                    const v8i fa = frag(A, frag_feature(wf, i) + (lane & 15));
-                    const float w = GATED && i >= kFragsF / 2 ? wa1 : wa;
-#pragma unroll
-                    for (int j = 0; j < kFragsR; ++j) {
+                    if constexpr (E4M3) {
+                        v4f sum[kFragsR];
                         const v4f zero = {0.0f, 0.0f, 0.0f, 0.0f};
-                        const v4f part = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa, fb[j], zero, 0, 0, 0, 0, 0, 0);
-                        const float f = scale[j] * w;
-#pragma unroll
-                        for (int t = 0; t < 4; ++t) acc[i][j][t] = fmaf(part[t], f, acc[i][j][t]);
-                    }
-                }
-            } else {
-                auto frag = [&](const char *T, bool trans, int first, int part) {
-                    if (trans) {
-                        const int f = first + (lane & 16), r = part * 16 + (lane >> 5) * 8;
-                        const v4s lo = read_transposed(T, r, f), hi = read_transposed(T, r + 4, f);
-                        const v8s both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-                        return __builtin_bit_cast(v8bf, both);
-                    }
-                    const int row = first + (lane & 31);
-                    return *(const v8bf *)(T + row * kStep + (((part * 2 + (lane >> 5)) ^ swizzle(row)) << 4));
-                };
-#pragma unroll
-                for (int part = 0; part < 4; ++part) {
-                    v8bf fa[kFragsF], fb[kFragsR];
-#pragma unroll
-                    for (int i = 0; i < kFragsF; ++i) fa[i] = frag(A, kTransA, frag_feature(wf, i), part);
-#pragma unroll
-                    for (int j = 0; j < kFragsR; ++j) fb[j] = frag(B, kTransB, (wr * kFragsR + j) * kSide, part);
-#pragma unroll
-                    for (int i = 0; i < kFragsF; ++i)
 #pragma unroll
                         for (int j = 0; j < kFragsR; ++j)
-                            acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[i], fb[j], acc[i][j], 0, 0, 0);
+                            sum[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa[i][part], b[j][part], zero, 0, 0, 0, 0, 0, 0);
+                        next(i, part);
+#pragma unroll
+                        for (int j = 0; j < kFragsR; ++j) {
+                            const float f = row_scale[g][j] * w;
+#pragma unroll
+                            for (int t = 0; t < 4; ++t) acc[h][g][i][j][t] = fmaf(sum[j][t], f, acc[h][g][i][j][t]);
+                        }
+                    } else {
+#pragma unroll
+                        for (int j = 0; j < kFragsR; ++j)
+                            acc[h][g][i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[i][part], b[j][part], acc[h][g][i][j], 0, 0, 0);
+                        next(i, part);
+                    }
                 }
-            }
         };
+        using Zero = std::integral_constant<int, 0>;
+        using One = std::integral_constant<int, 1>;
+        // Loads of this wave that may still be on their way between phases: all but the unit that the next phase reads
+        // and those before it, six units of two loads, and in e4m3 a load of scales or two among them.
+        constexpr int kAhead = E4M3 ? 13 : 12;
 
         __syncthreads();                           // the tile before is done with its LDS
-        if (steps) stage(0, 0);
-        for (int step = 0; step < steps; ++step) {
-            loads_done_and_barrier<0>();           // this step's operands are there, those of the step before are done with
-            if (step + 1 < steps) stage(step + 1, (step + 1) % STAGES);
-            multiply(step, step % STAGES);
+        load_scales(0); load(B0, 0); load(A0, 0); load(B1, 0); load(A1, 0);
+        load_scales(1); load(B0, 1); load(A0, 1); load(B1, 1); load(A1, 1);
+        loads_done_and_barrier<E4M3 ? 13 : 12>();
+#pragma unroll
+        for (int part = 0; part < kParts; ++part) {
+#pragma unroll
+            for (int i = 0; i < kFragsF; ++i) fa[i][part] = frag(U_A0(), Zero(), i, part);
+#pragma unroll
+            for (int j = 0; j < kFragsR; ++j) fb0[0][j][part] = frag(U_B0(), Zero(), j, part);
         }
+        loads_done_and_barrier<E4M3 ? 11 : 10>();
+        load(B0, 2); load_scales(2); load(A0, 2);
+
+        auto body = [&](int step, auto parity) {
+            constexpr int s = decltype(parity)::value;                 // step & 1
+            using S0 = std::integral_constant<int, s>;
+            using S1 = std::integral_constant<int, 1 - s>;
+            float w[2] = {0.0f, 0.0f};
+            if constexpr (E4M3) {
+                w[0] = sa[0][step]; w[1] = sa[1][step];
+                const float *S = (const float *)(lds + scales_at(step));
+#pragma unroll
+                for (int g = 0; g < 2; ++g)
+#pragma unroll
+                    for (int j = 0; j < kFragsR; ++j) row_scale[g][j] = S[g * 32 + j * kSide + (lane & 15)];
+            }
+            auto nothing = [](int, int) {};
+            // 1
+#pragma unroll
+            for (int part = 0; part < kParts; ++part)
+#pragma unroll
+                for (int j = 0; j < kFragsR; ++j) fb1[j][part] = frag(U_B1(), S0(), j, part);
+            multiply(Zero(), Zero(), fb0[s], w[0], nothing);
+            loads_done_and_barrier<kAhead>();
+            load(B1, step + 2);
+            // 2
+            multiply(Zero(), One(), fb1, w[0], [&](int i, int part) { fa[i][part] = frag(U_A1(), S0(), i, part); });
+            loads_done_and_barrier<kAhead>();
+            load(A1, step + 2);
+            // 3
+#pragma unroll
+            for (int part = 0; part < kParts; ++part)
+#pragma unroll
+                for (int j = 0; j < kFragsR; ++j) fb0[1 - s][j][part] = frag(U_B0(), S1(), j, part);
+            multiply(One(), One(), fb1, w[1], nothing);
+            loads_done_and_barrier<kAhead>();
+            load(B0, step + 3);
+            // 4
+            multiply(One(), Zero(), fb0[s], w[1], [&](int i, int part) { fa[i][part] = frag(U_A0(), S1(), i, part); });
+            loads_done_and_barrier<kAhead>();
+            load_scales(step + 3);
+            load(A0, step + 3);
+        };
+        for (int step = 0; step < steps; step += 2) {
+            body(step, Zero());
+            if (step + 1 < steps) body(step + 1, One());
+        }
+        loads_done_and_barrier<0>();               // also those of steps that are none
 
         // ---- the tile's output, 128 features at a time through LDS, so that rows are written in whole lines
         float *out = (float *)lds;
         const int piece = tid & 15, n_rows = n_b - r0 < ROWS ? n_b - r0 : ROWS;
-        // Moves value(i, j, t) of fragments [lo, hi) to LDS and from there, eight features a lane, to put(row, values).
-        auto emit = [&](int lo, int hi, auto value, auto put) {
+        // Moves value(g, i, j, t) of a half of the features to LDS and from there, eight features a lane, to put(row, values).
+        auto emit = [&](auto value, auto put) {
             __syncthreads();
 #pragma unroll
-            for (int i = 0; i < kFragsF; ++i) {
-                if (i < lo || i >= hi) continue;
-                const int f = frag_feature(wf, i) & (kHalf - 1);
+            for (int g = 0; g < kHalves; ++g)
 #pragma unroll
-                for (int j = 0; j < kFragsR; ++j) {
-                    const int row = (wr * kFragsR + j) * kSide + (lane & (kSide - 1));
+                for (int i = 0; i < kFragsF; ++i)
 #pragma unroll
-                    for (int t = 0; t < kAccs; t += 4) {
-                        const v4f v = {value(i, j, t), value(i, j, t + 1), value(i, j, t + 2), value(i, j, t + 3)};
-                        *(v4f *)(out + row * kEmitPitch + f + (E4M3 ? (lane >> 4) * 4 : t * 2 + (lane >> 5) * 4)) = v;
+                    for (int j = 0; j < kFragsR; ++j) {
+                        const int row = g * kHalf + wr * 32 + j * kSide + (lane & (kSide - 1)), f = wf * 64 + i * kSide;
+#pragma unroll
+                        for (int t = 0; t < kAccs; t += 4) {
+                            const v4f v = {value(g, i, j, t), value(g, i, j, t + 1), value(g, i, j, t + 2), value(g, i, j, t + 3)};
+                            *(v4f *)(out + row * kEmitPitch + f + (E4M3 ? (lane >> 4) * 4 : t * 2 + (lane >> 5) * 4)) = v;
+                        }
                     }
-                }
-            }
             __syncthreads();
             for (int row = tid >> 4; row < n_rows; row += kThreads / 16) {
                 const v4f x = *(const v4f *)(out + row * kEmitPitch + piece * 8), y = *(const v4f *)(out + row * kEmitPitch + piece * 8 + 4);
@@ -400,37 +466,32 @@ struct Tile {
             *(v2u *)((char *)to + row * width + f) = w;
             if (piece == 0) scales[row * (width / 128) + f / 128] = scale;
         };
-        // output row of the tile's row
+        // output row of the tile's first row
         const size_t row0 = FORM == kWeightGradient ? (size_t)e * P.other + r0 : (size_t)(rows.first + r0);
         const int f = f0 + piece * 8;
         if constexpr (GATED) {
-            auto gate = [&](int i, int j, int t) { return acc[i][j][t]; };
-            auto up = [&](int i, int j, int t) { return acc[i + kFragsF / 2 < kFragsF ? i + kFragsF / 2 : i][j][t]; };
             if (P.pre) {
-                for (int second = 0; second < 2; ++second) {
-                    auto keep = [&](int row, const float *v) {
-                        if (f >= P.features) return;
-                        if (P.pre_scales) put_e4m3(P.pre, P.pre_scales, row0 + row, second * P.features + f, 2 * P.features, v);
-                        else put_bf16(P.pre, row0 + row, second * P.features + f, 2 * P.features, v);
-                    };
-                    if (second) emit(0, kFragsF / 2, up, keep);
-                    else emit(0, kFragsF / 2, gate, keep);
-                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+                    emit([&](int g, int i, int j, int t) { return acc[h][g][i][j][t]; },
+                         [&](int row, const float *v) {
+                             if (f >= P.features) return;
+                             if (P.pre_scales) put_e4m3(P.pre, P.pre_scales, row0 + row, h * P.features + f, 2 * P.features, v);
+                             else put_bf16(P.pre, row0 + row, h * P.features + f, 2 * P.features, v);
+                         });
             }
-            emit(0, kFragsF / 2,
-                 [&](int i, int j, int t) { return activate<false>(P.act, gate(i, j, t), nullptr) * up(i, j, t); },
+            emit([&](int g, int i, int j, int t) { return activate<false>(P.act, acc[0][g][i][j][t], nullptr) * acc[1][g][i][j][t]; },
                  [&](int row, const float *v) {
                      if (f >= P.features) return;
                      if (E4M3) put_e4m3(P.out, P.out_scales, row0 + row, f, P.features, v);
                      else put_bf16(P.out, row0 + row, f, P.features, v);
                  });
         } else {
-            // a wave's features lie in one half: the waves of the other one wait at the barriers
 #pragma unroll
-            for (int half = 0; half < 2; ++half)
-                emit(frag_feature(wf, 0) / kHalf == half ? 0 : kFragsF, kFragsF, [&](int i, int j, int t) { return acc[i][j][t]; },
+            for (int h = 0; h < 2; ++h)
+                emit([&](int g, int i, int j, int t) { return acc[h][g][i][j][t]; },
                      [&](int row, const float *v) {
-                         if (f + half * kHalf < P.features) put_bf16(P.out, row0 + row, f + half * kHalf, P.features, v);
+                         if (f + h * kHalf < P.features) put_bf16(P.out, row0 + row, f + h * kHalf, P.features, v);
                      });
         }
     }
@@ -465,9 +526,9 @@ __device__ inline void scan_tiles(const Groups &G, int rows_per_tile, int *befor
 constexpr int kXcds = 8;
 constexpr int kRowGroup = 8;                   // row tiles that walk the features together
 
-template <int FORM, bool E4M3, bool GATED, int ROWS, int STAGES>
+template <int FORM, bool E4M3, bool GATED, int ROWS>
 __global__ __launch_bounds__(kThreads) void expert_tiles_kernel(Groups G, Product P) {
-    using T = Tile<FORM, E4M3, GATED, ROWS, STAGES>;
+    using T = Tile<FORM, E4M3, GATED, ROWS>;
     __shared__ __align__(1024) char lds[T::kLds];
     __shared__ int before[kMaxExperts + 1];
     const int columns = (P.features + T::kOutput - 1) / T::kOutput;
