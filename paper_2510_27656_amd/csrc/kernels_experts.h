@@ -25,7 +25,6 @@ typedef short v8s __attribute__((ext_vector_type(8)));
 typedef int v4i __attribute__((ext_vector_type(4)));
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
-typedef float v16f __attribute__((ext_vector_type(16)));
 typedef unsigned v2u __attribute__((ext_vector_type(2)));
 typedef unsigned v4u __attribute__((ext_vector_type(4)));
 
@@ -128,10 +127,19 @@ __device__ inline void to_lds_4(const Window &w, unsigned offset, unsigned shift
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds"
                  ::"s"(lds), "v"(offset), "s"(w.rsrc), "s"(shift) : "memory");
 }
-// Every load of this wave but the last KEEP is done, and so is every wave's, and its reads of LDS, behind the barrier.
+// The compiler keeps what comes before apart from what comes behind.
+__device__ inline void in_order() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+// Every load of this wave but the last KEEP is done, and so are its reads of LDS; behind the barrier every wave's.
+// (The compiler knows the wait's own form, so it does not wait for those reads again.)
 template <int KEEP>
 __device__ inline void loads_done_and_barrier() {
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(KEEP) : "memory");
+    in_order();
+    __builtin_amdgcn_s_waitcnt((KEEP & 15) | KEEP >> 4 << 14 | 7 << 4);      // vmcnt, lgkmcnt 0
+    __builtin_amdgcn_s_barrier();
+    in_order();
 }
 
 // ---------------------------------------------------------------- the tiles
@@ -169,16 +177,17 @@ struct Product {
 // Place of a 16-byte chunk in a unit, so that the lanes that are served together fall into different banks (64 of 4
 // bytes; sixteen lanes of a 16-byte read, 32 of an 8-byte one).
 // Contiguous along the contraction: rows of 128 bytes, chunk c of row r at c ^ (r >> 1 & 7): two rows fill the banks once.
-// Contiguous along the features: 64 contraction rows of 256 bytes, chunk c of row r at c ^ (r & 3) << 2: the transposing
-// reads take 64 bytes each of four rows at once.
+// Contiguous along the features: 64 contraction rows of 256 bytes; the transposing reads take 32 bytes each of rows
+// 8 m .. 8 m + 3 (or + 4) and of the same of the next eight rows at once, which the row's bits 0, 1 and 3 keep apart.
 __device__ inline int swizzle(int row) { return row >> 1 & 7; }
-__device__ inline int spread(int row) { return (row & 3) << 2; }
+__device__ inline int spread(int row) { return (row & 3) << 2 | (row >> 2 & 2); }
 
 template <int FORM, bool E4M3, bool GATED, int ROWS>
 struct Tile {
     static constexpr bool kTransA = FORM != kForward, kTransB = FORM == kWeightGradient;
-    static constexpr int kSide = E4M3 ? 16 : 32;                       // of a matrix instruction's output
-    static constexpr int kParts = E4M3 ? 1 : 4;                        // matrix instructions along a step
+    // Matrix instructions of 16 by 16 outputs, 64 bytes of bf16 or 128 of e4m3 deep.  (Alone on the machine they reach
+    // 2370 Tflop/s in bf16, 1930 with random operands; those of 32 by 32 outputs 1600 and 1310.)
+    static constexpr int kSide = 16, kParts = E4M3 ? 1 : 2;
     static constexpr int kFragsF = 64 / kSide, kFragsR = 32 / kSide;   // of a wave in a unit
     static constexpr int kHalves = ROWS / kHalf;
     static constexpr int kScales = E4M3 ? kWaves * kWave * 4 : 0;      // of a step: 64 rows' for each wave
@@ -187,14 +196,17 @@ struct Tile {
     static constexpr int kEmit = ROWS * kEmitPitch * 4;
     static constexpr int kLds = (kRing > kEmit ? kRing : kEmit) + kScaleSlots * kScales;
     static constexpr int kOutput = GATED ? kHalf : kFeatures;          // output features of a tile
-    using Acc = typename std::conditional<E4M3, v4f, v16f>::type;
+    using Acc = v4f;
     using Frag = typename std::conditional<E4M3, v8i, v8bf>::type;
-    static constexpr int kAccs = E4M3 ? 4 : 16;
     enum Unit { A0, A1, B0, B1 };
 
     // e: expert; rows: its rows; f0: first output feature; r0: first row (weight gradient: first column of b).
     __device__ static void run(const Product &P, char *lds, int e, const Rows &rows, int f0, int r0) {
-        const int tid = threadIdx.x, lane = tid & (kWave - 1), wave = __builtin_amdgcn_readfirstlane(tid / kWave);
+        // (opaque, so that what follows from it is worked out here and not kept in registers from tile to tile)
+        int tid = threadIdx.x;
+        asm volatile("" : "+v"(tid));
+        int lane = tid & (kWave - 1);
+        const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
         const int wf = wave & 1, wr = wave >> 1;
         const int size = E4M3 ? 1 : 2;
         const int k = FORM == kWeightGradient ? rows.n : P.k;          // contraction
@@ -206,7 +218,7 @@ struct Tile {
         unsigned off[2][4];                        // [operand][two loads of each unit]
         int steps_here[2];                         // steps in which this lane's chunk of a load is there (transposed: of both)
         const int chunk = (lane & 7) ^ swizzle(wave * 8 + (lane >> 3));           // as lies, contiguous along the contraction
-        const int column = ((lane & 15) ^ spread(lane >> 4)) * 8, depth = wave * 4 + (lane >> 4);   // transposed
+        const int depth = wave * 4 + (lane >> 4), column = ((lane & 15) ^ spread(depth)) * 8;       // transposed
 #pragma unroll
         for (int o = 0; o < 2; ++o) {
             const bool trans = o ? kTransB : kTransA;
@@ -272,26 +284,23 @@ struct Tile {
 
         // This wave's fragments of a unit.  Their places differ from the first one's by constants and, where the swizzle
         // reaches into them, by one of a few patterns: those are kept as addresses.
-        //   bf16: 8 values of a row from chunk 2 part + (lane >> 5) on; a pattern for each part
-        //   e4m3: chunks lane >> 4 and that plus 4 (any order of the contraction will do that both operands have)
-        //   transposed: lanes 16 i .. 16 i + 15 give the places of four rows by four pieces of 8 bytes, and lane j of them
+        //   contiguous along the contraction: chunks lane >> 4 and that plus 4 of row lane & 15, bf16 one for each of two
+        //   instructions, e4m3 both for one (any order of the contraction will do that both operands have)
+        //   transposed: lanes 16 m .. 16 m + 15 give the places of four rows by four pieces of 8 bytes, and lane j of them
         //   receives column j; a pattern for each fragment
-        constexpr int kPatterns = 4;
+        constexpr int kPatterns = kTransA || kTransB ? 4 : 2;
         unsigned at[2][kPatterns];
 #pragma unroll
         for (int o = 0; o < 2; ++o) {
             const int first = o ? wr * 32 : wf * 64, unit = lds0 + place(o ? B0 : A0, 0);
 #pragma unroll
             for (int p = 0; p < kPatterns; ++p) {
-                if (E4M3) {
-                    const int row = lane & 15;
-                    at[o][p] = unit + (first + row) * kStep + (((lane >> 4) + (p & 1) * 4) ^ swizzle(row)) * 16;
-                } else if (o ? kTransB : kTransA) {
-                    const int row = (lane >> 5) * 8 + (lane >> 2 & 3), c = (first + p * kSide + (lane & 16)) / 8 + (lane >> 1 & 1);
+                if (o ? kTransB : kTransA) {
+                    const int row = (lane >> 4) * 8 + (lane >> 2 & 3), c = (first + p * kSide) / 8 + (lane >> 1 & 1);
                     at[o][p] = unit + row * 256 + (c ^ spread(row)) * 16 + (lane & 1) * 8;
                 } else {
-                    const int row = lane & 31;
-                    at[o][p] = unit + (first + row) * kStep + ((p * 2 + (lane >> 5)) ^ swizzle(row)) * 16;
+                    const int row = lane & 15;
+                    at[o][p] = unit + (first + row) * kStep + (((lane >> 4) + (p & 1) * 4) ^ swizzle(row)) * 16;
                 }
                 asm volatile("" : "+v"(at[o][p]));                     // not to be worked out again at every use
             }
@@ -303,8 +312,8 @@ struct Tile {
                 const v4i hi = *(FLMOE_LDS const v4i *)(uintptr_t)(at[o][1] + base + i * kSide * kStep);
                 return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
             } else if constexpr (o ? kTransB : kTransA) {
-                const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((FLMOE_LDS v4s *)(uintptr_t)(at[o][i] + base + part * 4096));
-                const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((FLMOE_LDS v4s *)(uintptr_t)(at[o][i] + base + part * 4096 + 1024));
+                const v4s lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((FLMOE_LDS v4s *)(uintptr_t)(at[o][i] + base + part * 8192));
+                const v4s hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((FLMOE_LDS v4s *)(uintptr_t)(at[o][i] + base + part * 8192 + 1024));
                 const v8s both = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
                 return __builtin_bit_cast(v8bf, both);
             } else {
@@ -326,37 +335,47 @@ struct Tile {
 #pragma unroll
                     for (int j = 0; j < kFragsR; ++j)
 #pragma unroll
-                        for (int t = 0; t < kAccs; ++t) acc[h][g][i][j][t] = 0.0f;
+                        for (int t = 0; t < 4; ++t) acc[h][g][i][j][t] = 0.0f;
 
         Frag fa[kFragsF][kParts], fb0[2][kFragsR][kParts], fb1[kFragsR][kParts];
-        float row_scale[2][kFragsR];
+        float row_scale[kFragsR];
         // multiplies the fragments at hand into quadrant (h, g); next(i, part) follows a fragment's last use
         auto multiply = [&](auto half_a, auto half_b, const Frag (&b)[kFragsR][kParts], float w, auto next) {
             constexpr int h = decltype(half_a)::value, g = decltype(half_b)::value;
+            if constexpr (E4M3) {
+                // a block's sum enters the accumulators, times both scales, while the next fragment's is on its way
+                v4f sum[2][kFragsR];
+                auto add = [&](int i) {
 #pragma unroll
-            for (int part = 0; part < kParts; ++part)
+                    for (int j = 0; j < kFragsR; ++j) {
+                        const float f = row_scale[j] * w;
+#pragma unroll
+                        for (int t = 0; t < 4; ++t) acc[h][g][i][j][t] = fmaf(sum[i & 1][j][t], f, acc[h][g][i][j][t]);
+                    }
+                };
 #pragma unroll
                 for (int i = 0; i < kFragsF; ++i) {
-                    if constexpr (E4M3) {
-                        v4f sum[kFragsR];
-                        const v4f zero = {0.0f, 0.0f, 0.0f, 0.0f};
+                    const v4f zero = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-                        for (int j = 0; j < kFragsR; ++j)
-                            sum[j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa[i][part], b[j][part], zero, 0, 0, 0, 0, 0, 0);
-                        next(i, part);
-#pragma unroll
-                        for (int j = 0; j < kFragsR; ++j) {
-                            const float f = row_scale[g][j] * w;
-#pragma unroll
-                            for (int t = 0; t < 4; ++t) acc[h][g][i][j][t] = fmaf(sum[j][t], f, acc[h][g][i][j][t]);
-                        }
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < kFragsR; ++j)
-                            acc[h][g][i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[i][part], b[j][part], acc[h][g][i][j], 0, 0, 0);
-                        next(i, part);
-                    }
+                    for (int j = 0; j < kFragsR; ++j)
+                        sum[i & 1][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa[i][0], b[j][0], zero, 0, 0, 0, 0, 0, 0);
+                    next(i, 0);
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (i) add(i - 1);
                 }
+                add(kFragsF - 1);
+            } else {
+#pragma unroll
+                for (int part = 0; part < kParts; ++part)
+#pragma unroll
+                    for (int i = 0; i < kFragsF; ++i) {
+#pragma unroll
+                        for (int j = 0; j < kFragsR; ++j)
+                            acc[h][g][i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fa[i][part], b[j][part], acc[h][g][i][j], 0, 0, 0);
+                        next(i, part);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+            }
         };
         using Zero = std::integral_constant<int, 0>;
         using One = std::integral_constant<int, 1>;
@@ -384,23 +403,30 @@ struct Tile {
             using S1 = std::integral_constant<int, 1 - s>;
             float w[2] = {0.0f, 0.0f};
             if constexpr (E4M3) {
-                w[0] = sa[0][step]; w[1] = sa[1][step];
-                const float *S = (const float *)(lds + scales_at(step));
-#pragma unroll
-                for (int g = 0; g < 2; ++g)
-#pragma unroll
-                    for (int j = 0; j < kFragsR; ++j) row_scale[g][j] = S[g * 32 + j * kSide + (lane & 15)];
+                const int there = s && step >= steps ? step - 1 : step;
+                w[0] = sa[0][there]; w[1] = sa[1][there];
+                if (s && step >= steps) w[0] = w[1] = 0.0f;
             }
+            auto scales_of = [&](int g) {                              // of the rows of a unit of B
+                if constexpr (E4M3) {
+                    const float *S = (const float *)(lds + scales_at(step)) + g * 32 + (lane & 15);
+#pragma unroll
+                    for (int j = 0; j < kFragsR; ++j) row_scale[j] = S[j * kSide];
+                }
+            };
             auto nothing = [](int, int) {};
             // 1
 #pragma unroll
             for (int part = 0; part < kParts; ++part)
 #pragma unroll
                 for (int j = 0; j < kFragsR; ++j) fb1[j][part] = frag(U_B1(), S0(), j, part);
+            in_order();
+            scales_of(0);
             multiply(Zero(), Zero(), fb0[s], w[0], nothing);
             loads_done_and_barrier<kAhead>();
             load(B1, step + 2);
             // 2
+            scales_of(1);
             multiply(Zero(), One(), fb1, w[0], [&](int i, int part) { fa[i][part] = frag(U_A1(), S0(), i, part); });
             loads_done_and_barrier<kAhead>();
             load(A1, step + 2);
@@ -409,23 +435,28 @@ struct Tile {
             for (int part = 0; part < kParts; ++part)
 #pragma unroll
                 for (int j = 0; j < kFragsR; ++j) fb0[1 - s][j][part] = frag(U_B0(), S1(), j, part);
+            in_order();
             multiply(One(), One(), fb1, w[1], nothing);
             loads_done_and_barrier<kAhead>();
             load(B0, step + 3);
             // 4
+            scales_of(0);
             multiply(One(), Zero(), fb0[s], w[1], [&](int i, int part) { fa[i][part] = frag(U_A0(), S1(), i, part); });
             loads_done_and_barrier<kAhead>();
             load_scales(step + 3);
             load(A0, step + 3);
         };
-        for (int step = 0; step < steps; step += 2) {
+        for (int step = 0; step < steps; step += 2) {                  // behind an odd last step, one of zeros
             body(step, Zero());
-            if (step + 1 < steps) body(step + 1, One());
+            body(step + 1, One());
         }
         loads_done_and_barrier<0>();               // also those of steps that are none
 
         // ---- the tile's output, 128 features at a time through LDS, so that rows are written in whole lines
         float *out = (float *)lds;
+        tid = threadIdx.x;
+        asm volatile("" : "+v"(tid));
+        lane = tid & (kWave - 1);
         const int piece = tid & 15, n_rows = n_b - r0 < ROWS ? n_b - r0 : ROWS;
         // Moves value(g, i, j, t) of a half of the features to LDS and from there, eight features a lane, to put(row, values).
         auto emit = [&](auto value, auto put) {
@@ -436,12 +467,9 @@ struct Tile {
                 for (int i = 0; i < kFragsF; ++i)
 #pragma unroll
                     for (int j = 0; j < kFragsR; ++j) {
-                        const int row = g * kHalf + wr * 32 + j * kSide + (lane & (kSide - 1)), f = wf * 64 + i * kSide;
-#pragma unroll
-                        for (int t = 0; t < kAccs; t += 4) {
-                            const v4f v = {value(g, i, j, t), value(g, i, j, t + 1), value(g, i, j, t + 2), value(g, i, j, t + 3)};
-                            *(v4f *)(out + row * kEmitPitch + f + (E4M3 ? (lane >> 4) * 4 : t * 2 + (lane >> 5) * 4)) = v;
-                        }
+                        const int row = g * kHalf + wr * 32 + j * kSide + (lane & 15), f = wf * 64 + i * kSide + (lane >> 4) * 4;
+                        const v4f v = {value(g, i, j, 0), value(g, i, j, 1), value(g, i, j, 2), value(g, i, j, 3)};
+                        *(v4f *)(out + row * kEmitPitch + f) = v;
                     }
             __syncthreads();
             for (int row = tid >> 4; row < n_rows; row += kThreads / 16) {
