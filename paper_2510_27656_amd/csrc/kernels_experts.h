@@ -213,8 +213,8 @@ struct Tile {
         const int n_b = FORM == kWeightGradient ? P.other : rows.n;    // rows of operand b
         const int steps = (int)(((long long)k * size + kStep - 1) / kStep);
 
-        // Where this lane's chunks come from.  Features and rows past the end are replaced by ones that are there (what
-        // is computed from them is not written), the contraction's by zeros.
+        // Where this lane's chunks come from.  Past the end of the features there are others that are as good (what is
+        // computed from them is not written); past the rows and past the contraction there are zeros.
         unsigned off[2][4];                        // [operand][two loads of each unit]
         int steps_here[2];                         // steps in which this lane's chunk of a load is there (transposed: of both)
         const int chunk = (lane & 7) ^ swizzle(wave * 8 + (lane >> 3));           // as lies, contiguous along the contraction
@@ -226,14 +226,12 @@ struct Tile {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 if (trans) {
-                    int f = (j >> 1) * kHalf + column;
-                    if (f >= end) f = 0;
-                    off[o][j] = (unsigned)(depth + (j & 1) * 32) * ld + f * 2;
+                    const int f = (j >> 1) * kHalf + column;
+                    off[o][j] = (unsigned)(depth + (j & 1) * 32) * ld + (f < end ? f : 0) * 2;
                 } else {
                     int r = (j * kWaves + wave) * 8 + (lane >> 3);
                     if (!o && GATED) r &= kHalf - 1;
-                    if (r >= end) r = 0;
-                    off[o][j] = (unsigned)r * ld + chunk * 16;
+                    off[o][j] = r < end ? (unsigned)r * ld + chunk * 16 : o ? kNowhere : (unsigned)chunk * 16;
                 }
             }
             steps_here[o] = trans ? (k - depth + 63) / 64 : (k * size - chunk * 16 + kStep - 1) / kStep;
@@ -379,76 +377,127 @@ struct Tile {
         };
         using Zero = std::integral_constant<int, 0>;
         using One = std::integral_constant<int, 1>;
-        // Loads of this wave that may still be on their way between phases: all but the unit that the next phase reads
-        // and those before it, six units of two loads, and in e4m3 a load of scales or two among them.
-        constexpr int kAhead = E4M3 ? 13 : 12;
+        auto nothing = [](int, int) {};
+        // What one wave does for step `step`; s: step & 1.
+        float w[2] = {0.0f, 0.0f};
+        auto scales_of_weights = [&](int step, auto parity) {
+            if constexpr (E4M3) {
+                const bool there = !parity() || step < steps;          // behind an odd last step there is one of zeros
+                w[0] = sa[0][there ? step : step - 1]; w[1] = sa[1][there ? step : step - 1];
+                if (!there) w[0] = w[1] = 0.0f;
+            }
+        };
+        auto scales_of = [&](int step, int g) {                        // of the rows of a unit of B
+            if constexpr (E4M3) {
+                const float *S = (const float *)(lds + scales_at(step)) + g * 32 + (lane & 15);
+#pragma unroll
+                for (int j = 0; j < kFragsR; ++j) row_scale[j] = S[j * kSide];
+            }
+        };
+        auto read_b = [&](Frag (&to)[kFragsR][kParts], auto unit, auto slot) {
+#pragma unroll
+            for (int part = 0; part < kParts; ++part)
+#pragma unroll
+                for (int j = 0; j < kFragsR; ++j) to[j][part] = frag(unit, slot, j, part);
+        };
+        auto read_a = [&] {
+#pragma unroll
+            for (int part = 0; part < kParts; ++part)
+#pragma unroll
+                for (int i = 0; i < kFragsF; ++i) fa[i][part] = frag(U_A0(), Zero(), i, part);
+        };
 
         __syncthreads();                           // the tile before is done with its LDS
-        load_scales(0); load(B0, 0); load(A0, 0); load(B1, 0); load(A1, 0);
-        load_scales(1); load(B0, 1); load(A0, 1); load(B1, 1); load(A1, 1);
-        loads_done_and_barrier<E4M3 ? 13 : 12>();
-#pragma unroll
-        for (int part = 0; part < kParts; ++part) {
-#pragma unroll
-            for (int i = 0; i < kFragsF; ++i) fa[i][part] = frag(U_A0(), Zero(), i, part);
-#pragma unroll
-            for (int j = 0; j < kFragsR; ++j) fb0[0][j][part] = frag(U_B0(), Zero(), j, part);
-        }
-        loads_done_and_barrier<E4M3 ? 11 : 10>();
-        load(B0, 2); load_scales(2); load(A0, 2);
-
-        auto body = [&](int step, auto parity) {
-            constexpr int s = decltype(parity)::value;                 // step & 1
-            using S0 = std::integral_constant<int, s>;
-            using S1 = std::integral_constant<int, 1 - s>;
-            float w[2] = {0.0f, 0.0f};
-            if constexpr (E4M3) {
-                const int there = s && step >= steps ? step - 1 : step;
-                w[0] = sa[0][there]; w[1] = sa[1][there];
-                if (s && step >= steps) w[0] = w[1] = 0.0f;
-            }
-            auto scales_of = [&](int g) {                              // of the rows of a unit of B
-                if constexpr (E4M3) {
-                    const float *S = (const float *)(lds + scales_at(step)) + g * 32 + (lane & 15);
-#pragma unroll
-                    for (int j = 0; j < kFragsR; ++j) row_scale[j] = S[j * kSide];
-                }
+        if (n_b - r0 > kHalf) {
+            // Loads of this wave that may still be on their way between phases: all but the unit that the next phase reads
+            // and those before it, six units of two loads, and in e4m3 a load of scales or two among them.
+            constexpr int kAhead = E4M3 ? 13 : 12;
+            load_scales(0); load(B0, 0); load(A0, 0); load(B1, 0); load(A1, 0);
+            load_scales(1); load(B0, 1); load(A0, 1); load(B1, 1); load(A1, 1);
+            loads_done_and_barrier<kAhead>();
+            read_a();
+            read_b(fb0[0], U_B0(), Zero());
+            loads_done_and_barrier<kAhead - 2>();
+            load(B0, 2); load_scales(2); load(A0, 2);
+            auto body = [&](int step, auto parity) {
+                constexpr int s = parity();
+                using S0 = std::integral_constant<int, s>;
+                using S1 = std::integral_constant<int, 1 - s>;
+                scales_of_weights(step, parity);
+                // 1
+                scales_of(step, 0);
+                read_b(fb1, U_B1(), S0());
+                in_order();
+                multiply(Zero(), Zero(), fb0[s], w[0], nothing);
+                loads_done_and_barrier<kAhead>();
+                load(B1, step + 2);
+                // 2
+                scales_of(step, 1);
+                multiply(Zero(), One(), fb1, w[0], [&](int i, int part) { fa[i][part] = frag(U_A1(), S0(), i, part); });
+                loads_done_and_barrier<kAhead>();
+                load(A1, step + 2);
+                // 3
+                read_b(fb0[1 - s], U_B0(), S1());
+                in_order();
+                multiply(One(), One(), fb1, w[1], nothing);
+                loads_done_and_barrier<kAhead>();
+                load(B0, step + 3);
+                // 4
+                scales_of(step, 0);
+                multiply(One(), Zero(), fb0[s], w[1], [&](int i, int part) { fa[i][part] = frag(U_A0(), S1(), i, part); });
+                loads_done_and_barrier<kAhead>();
+                load_scales(step + 3);
+                load(A0, step + 3);
             };
-            auto nothing = [](int, int) {};
-            // 1
-#pragma unroll
-            for (int part = 0; part < kParts; ++part)
-#pragma unroll
-                for (int j = 0; j < kFragsR; ++j) fb1[j][part] = frag(U_B1(), S0(), j, part);
-            in_order();
-            scales_of(0);
-            multiply(Zero(), Zero(), fb0[s], w[0], nothing);
-            loads_done_and_barrier<kAhead>();
-            load(B1, step + 2);
-            // 2
-            scales_of(1);
-            multiply(Zero(), One(), fb1, w[0], [&](int i, int part) { fa[i][part] = frag(U_A1(), S0(), i, part); });
-            loads_done_and_barrier<kAhead>();
-            load(A1, step + 2);
-            // 3
-#pragma unroll
-            for (int part = 0; part < kParts; ++part)
-#pragma unroll
-                for (int j = 0; j < kFragsR; ++j) fb0[1 - s][j][part] = frag(U_B0(), S1(), j, part);
-            in_order();
-            multiply(One(), One(), fb1, w[1], nothing);
-            loads_done_and_barrier<kAhead>();
-            load(B0, step + 3);
-            // 4
-            scales_of(0);
-            multiply(One(), Zero(), fb0[s], w[1], [&](int i, int part) { fa[i][part] = frag(U_A0(), S1(), i, part); });
-            loads_done_and_barrier<kAhead>();
-            load_scales(step + 3);
-            load(A0, step + 3);
-        };
-        for (int step = 0; step < steps; step += 2) {                  // behind an odd last step, one of zeros
-            body(step, Zero());
-            body(step + 1, One());
+            for (int step = 0; step < steps; step += 2) {              // behind an odd last step, one of zeros
+                body(step, Zero());
+                body(step + 1, One());
+            }
+        } else {
+            // At most 128 rows: no B1, two phases.  Waves whose 32 rows there are none of only load.
+            constexpr int kAhead = E4M3 ? 7 : 6;
+            load_scales(0); load(B0, 0); load(A0, 0); load(A1, 0);
+            load_scales(1); load(B0, 1); load(A0, 1); load(A1, 1);
+            loads_done_and_barrier<kAhead + 2>();
+            auto start = [&] {
+                loads_done_and_barrier<kAhead>();
+                load(B0, 2); load_scales(2); load(A0, 2);
+            };
+            auto body = [&](int step, auto parity, auto present) {
+                constexpr int s = parity();
+                constexpr bool here = present();
+                using S0 = std::integral_constant<int, s>;
+                using S1 = std::integral_constant<int, 1 - s>;
+                if constexpr (here) {
+                    scales_of_weights(step, parity);
+                    scales_of(step, 0);
+                    multiply(Zero(), Zero(), fb0[s], w[0], [&](int i, int part) { fa[i][part] = frag(U_A1(), S0(), i, part); });
+                }
+                loads_done_and_barrier<kAhead>();
+                load(A1, step + 2);
+                if constexpr (here) {
+                    read_b(fb0[1 - s], U_B0(), S1());
+                    in_order();
+                    multiply(One(), Zero(), fb0[s], w[1], [&](int i, int part) { fa[i][part] = frag(U_A0(), S1(), i, part); });
+                }
+                loads_done_and_barrier<kAhead>();
+                load(B0, step + 3); load_scales(step + 3); load(A0, step + 3);
+            };
+            if (wr * 32 < n_b - r0) {
+                read_a();
+                read_b(fb0[0], U_B0(), Zero());
+                start();
+                for (int step = 0; step < steps; step += 2) {
+                    body(step, Zero(), One());
+                    body(step + 1, One(), One());
+                }
+            } else {
+                start();
+                for (int step = 0; step < steps; step += 2) {
+                    body(step, Zero(), Zero());
+                    body(step + 1, One(), Zero());
+                }
+            }
         }
         loads_done_and_barrier<0>();               // also those of steps that are none
 
