@@ -14,6 +14,7 @@ namespace flmoe {
 namespace experts {
 
 constexpr int kMaxWidth = 1 << 20;             // as fl_moe_config.hidden
+constexpr long long kFewRows = 32;             // see launch_tiles
 constexpr int kUnits = 256;                    // compute units of the part
 
 // What a call's configuration and tables come to.
@@ -28,6 +29,10 @@ inline int groups_of(const fl_moe_config *cfg, int rank_begin, int rank_count, c
     const int El = cfg->n_experts / cfg->n_ranks;
     *G = Groups{El, rank_begin * El, rank_count * El, sizes.expert_capacity_rows, expert_off, tokens_per_expert};
     return FL_OK;
+}
+
+inline long long mean_rows(const fl_moe_config *cfg, const Groups &G) {
+    return std::max(1ll, (long long)cfg->max_tokens * cfg->top_k / G.El);
 }
 
 inline int check_width(int width, int multiple) {
@@ -58,10 +63,29 @@ inline int compute_units() {
 
 inline int launched() { return hipGetLastError() == hipSuccess ? FL_OK : FL_ERR_HIP; }
 
+// mean: rows an expert would have if the tokens of the configuration were spread evenly.
 template <int FORM, bool E4M3, bool GATED>
-int launch_tiles(const Groups &G, const Product &P, hipStream_t st) {
-    const int grid = std::max(1, compute_units() / kXcds) * kXcds;
-    expert_tiles_kernel<FORM, E4M3, GATED, 256><<<dim3(grid), dim3(kThreads), 0, st>>>(G, P);
+int launch_tiles(const Groups &G, long long mean, const Product &P, hipStream_t st) {
+    const int units = std::max(1, compute_units() / kXcds) * kXcds;
+    auto go = [&](auto rows, auto half, int per_unit) {
+        using T = Tile<FORM, E4M3, GATED, rows(), half()>;
+        expert_tiles_kernel<FORM, E4M3, GATED, rows(), half()><<<dim3(units * per_unit), dim3(T::kThreads), 0, st>>>(G, P);
+    };
+    using std::integral_constant;
+    if constexpr (FORM == kForward) {
+        if (mean <= kFewRows) {
+            // (what answers in blocks of 128 features has to have them in one tile)
+            if constexpr (GATED) {
+                if (E4M3 || P.pre_scales) {
+                    go(integral_constant<int, 32>(), integral_constant<int, 128>(), 1);
+                    return launched();
+                }
+            }
+            if constexpr (!(E4M3 && GATED)) go(integral_constant<int, 32>(), integral_constant<int, 64>(), P.k * (E4M3 ? 1 : 2) <= 2048 ? 3 : 2);
+            return launched();
+        }
+    }
+    go(integral_constant<int, 256>(), integral_constant<int, 128>(), 1);
     return launched();
 }
 
@@ -113,7 +137,7 @@ int fl_moe_expert_gated(const fl_moe_config *cfg, int rb, int rc, const int32_t 
     Product P = forward(x, w, h, cfg->hidden, inter);
     P.a_expert *= 2;
     P.pre = pre; P.pre_scales = pre_scales; P.act = activation;
-    return launch_tiles<kForward, false, true>(G, P, (hipStream_t)stream);
+    return launch_tiles<kForward, false, true>(G, mean_rows(cfg, G), P, (hipStream_t)stream);
 }
 
 int fl_moe_expert_gated_backward(const fl_moe_config *cfg, int rb, int rc, const int32_t *expert_off,
@@ -130,13 +154,13 @@ int fl_moe_expert_gated_backward(const fl_moe_config *cfg, int rb, int rc, const
     if (((uintptr_t)x | (uintptr_t)w | (uintptr_t)dx | (uintptr_t)dw | (uintptr_t)h) & 15 || (uintptr_t)pre_scales & 3)
         return FL_ERR_ALIGNMENT;
     hipStream_t st = (hipStream_t)stream;
-    const long long mean = std::max(1ll, (long long)cfg->max_tokens * cfg->top_k / G.El);       // rows of an expert
+    const long long mean = mean_rows(cfg, G);
     const long long blocks = std::min(std::max(1ll, (mean * (inter / 8) + 1023) / 1024), (1ll << 18) / G.n);
     expert_gated_gradient_kernel<<<dim3((unsigned)blocks, G.n), dim3(256), 0, st>>>(
         G, inter, activation, (const char *)pre, pre_scales, (const char *)dh, (char *)dpre, (char *)h);
     FL_CHECK(launched());
-    if (dx) FL_CHECK((launch_tiles<kRowGradient, false, false>(G, row_gradient(dpre, w, dx, cfg->hidden, 2 * inter), st)));
-    if (dw) FL_CHECK((launch_tiles<kWeightGradient, false, false>(G, weight_gradient(dpre, x, dw, cfg->hidden, 2 * inter), st)));
+    if (dx) FL_CHECK((launch_tiles<kRowGradient, false, false>(G, 0, row_gradient(dpre, w, dx, cfg->hidden, 2 * inter), st)));
+    if (dw) FL_CHECK((launch_tiles<kWeightGradient, false, false>(G, 0, weight_gradient(dpre, x, dw, cfg->hidden, 2 * inter), st)));
     return FL_OK;
 }
 
@@ -148,7 +172,7 @@ int fl_moe_expert_product(const fl_moe_config *cfg, int rb, int rc, const int32_
     FL_CHECK(check_width(in, 8));
     FL_CHECK(check_width(out, 8));
     FL_CHECK(check_tensors({x, w, y}));
-    return launch_tiles<kForward, false, false>(G, forward(x, w, y, in, out), (hipStream_t)stream);
+    return launch_tiles<kForward, false, false>(G, mean_rows(cfg, G), forward(x, w, y, in, out), (hipStream_t)stream);
 }
 
 int fl_moe_expert_product_backward(const fl_moe_config *cfg, int rb, int rc, const int32_t *expert_off,
@@ -163,8 +187,8 @@ int fl_moe_expert_product_backward(const fl_moe_config *cfg, int rb, int rc, con
     if ((!dx && !dw) || (dx && !w) || (dw && !x)) return FL_ERR_INVALID_ARG;
     if (((uintptr_t)x | (uintptr_t)w | (uintptr_t)dx | (uintptr_t)dw) & 15) return FL_ERR_ALIGNMENT;
     hipStream_t st = (hipStream_t)stream;
-    if (dx) FL_CHECK((launch_tiles<kRowGradient, false, false>(G, row_gradient(dy, w, dx, in, out), st)));
-    if (dw) FL_CHECK((launch_tiles<kWeightGradient, false, false>(G, weight_gradient(dy, x, dw, in, out), st)));
+    if (dx) FL_CHECK((launch_tiles<kRowGradient, false, false>(G, 0, row_gradient(dy, w, dx, in, out), st)));
+    if (dw) FL_CHECK((launch_tiles<kWeightGradient, false, false>(G, 0, weight_gradient(dy, x, dw, in, out), st)));
     return FL_OK;
 }
 
@@ -184,7 +208,7 @@ int fl_moe_expert_gated_e4m3(const fl_moe_config *cfg, int rb, int rc, const int
     P.a_ld = P.b_ld = P.k = cfg->hidden;
     P.features = inter;
     P.a_expert = 2ll * inter * cfg->hidden;
-    return launch_tiles<kForward, true, true>(G, P, (hipStream_t)stream);
+    return launch_tiles<kForward, true, true>(G, mean_rows(cfg, G), P, (hipStream_t)stream);
 }
 
 int fl_moe_expert_product_e4m3(const fl_moe_config *cfg, int rb, int rc, const int32_t *expert_off,
@@ -202,7 +226,7 @@ int fl_moe_expert_product_e4m3(const fl_moe_config *cfg, int rb, int rc, const i
     P.a_ld = P.b_ld = P.k = in;
     P.features = out;
     P.a_expert = (long long)out * in;
-    return launch_tiles<kForward, true, false>(G, P, (hipStream_t)stream);
+    return launch_tiles<kForward, true, false>(G, mean_rows(cfg, G), P, (hipStream_t)stream);
 }
 
 }  // extern "C"

@@ -121,11 +121,11 @@ struct Window {
 __device__ inline unsigned lds_address(const char *lds) { return (unsigned)(uintptr_t)(FLMOE_LDS const char *)lds; }
 __device__ inline void to_lds_16(const Window &w, unsigned offset, unsigned shift, unsigned lds) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
-                 ::"s"(lds), "v"(offset), "s"(w.rsrc), "s"(shift) : "memory");
+                 ::"s"(__builtin_amdgcn_readfirstlane((int)lds)), "v"(offset), "s"(w.rsrc), "s"(__builtin_amdgcn_readfirstlane((int)shift)) : "memory");
 }
 __device__ inline void to_lds_4(const Window &w, unsigned offset, unsigned shift, unsigned lds) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds"
-                 ::"s"(lds), "v"(offset), "s"(w.rsrc), "s"(shift) : "memory");
+                 ::"s"(__builtin_amdgcn_readfirstlane((int)lds)), "v"(offset), "s"(w.rsrc), "s"(__builtin_amdgcn_readfirstlane((int)shift)) : "memory");
 }
 // The compiler keeps what comes before apart from what comes behind.
 __device__ inline void in_order() {
@@ -152,12 +152,8 @@ __device__ inline void loads_done_and_barrier() {
 // So a unit's LDS is free again one phase after it was first touched, and with two places for each unit the loads that
 // fill it have almost two steps to arrive: 128 KB are on their way to a compute unit nearly all the time.  Between
 // phases: this wave's reads are done, its oldest loads have arrived, barrier.
-constexpr int kThreads = 512, kWaves = kThreads / kWave;
 constexpr int kStep = 128;                     // bytes of the contraction per step
-constexpr int kHalf = 128;                     // features, or rows, of a unit
-constexpr int kUnit = kHalf * kStep;
-constexpr int kFeatures = 2 * kHalf;
-constexpr int kEmitPitch = kHalf + 4;          // floats from row to row of the tile's output in LDS
+constexpr int kXcds = 8;
 
 enum Form { kForward, kRowGradient, kWeightGradient };
 
@@ -182,20 +178,30 @@ struct Product {
 __device__ inline int swizzle(int row) { return row >> 1 & 7; }
 __device__ inline int spread(int row) { return (row & 3) << 2 | (row >> 2 & 2); }
 
-template <int FORM, bool E4M3, bool GATED, int ROWS>
+// ROWS: 256, or 32 for experts of few rows, with HALF features to a unit of A (a wave for every 16 of them).
+template <int FORM, bool E4M3, bool GATED, int ROWS, int HALF>
 struct Tile {
     static constexpr bool kTransA = FORM != kForward, kTransB = FORM == kWeightGradient;
+    static_assert((ROWS == 256 && HALF == 128) || (ROWS == 32 && FORM == kForward && (HALF == 128 || HALF == 64)), "");
+    static constexpr int kThreads = ROWS == 256 ? 512 : HALF * 4, kWaves = kThreads / kWave;
     // Matrix instructions of 16 by 16 outputs, 64 bytes of bf16 or 128 of e4m3 deep.  (Alone on the machine they reach
     // 2370 Tflop/s in bf16, 1930 with random operands; those of 32 by 32 outputs 1600 and 1310.)
     static constexpr int kSide = 16, kParts = E4M3 ? 1 : 2;
-    static constexpr int kFragsF = 64 / kSide, kFragsR = 32 / kSide;   // of a wave in a unit
-    static constexpr int kHalves = ROWS / kHalf;
-    static constexpr int kScales = E4M3 ? kWaves * kWave * 4 : 0;      // of a step: 64 rows' for each wave
-    static constexpr int kScaleSlots = 4;
-    static constexpr int kRing = 2 * (2 + kHalves) * kUnit;            // [two][A0, A1, B0, B1]
+    static constexpr int kHalves = ROWS == 256 ? 2 : 1;                // units of B
+    static constexpr int kUnitRows = ROWS / kHalves, kUnitA = HALF * kStep, kUnitB = kUnitRows * kStep;
+    static constexpr int kWavesF = ROWS == 256 ? 2 : kWaves, kWavesR = kWaves / kWavesF;
+    static constexpr int kOwnF = HALF / kWavesF, kOwnR = kUnitRows / kWavesR;         // of a wave in a unit
+    static constexpr int kFragsF = kOwnF / kSide, kFragsR = kOwnR / kSide;
+    static constexpr int kLoadsB = ROWS == 256 ? 2 : 1;                // of a wave for a unit of B
+    static constexpr int kLoadRowsB = kUnitRows / kWaves / kLoadsB;    // ... of 8 rows each, or of 4 by half the lanes
+    static constexpr int kRing = 4 * kUnitA + 2 * kHalves * kUnitB;    // [two][A0, A1], [two][B0, B1]
+    static constexpr int kEmitPitch = HALF + 4;                        // floats from row to row of the output in LDS
     static constexpr int kEmit = ROWS * kEmitPitch * 4;
-    static constexpr int kLds = (kRing > kEmit ? kRing : kEmit) + kScaleSlots * kScales;
-    static constexpr int kOutput = GATED ? kHalf : kFeatures;          // output features of a tile
+    // scales of the rows of a step: those of its own rows for each wave, or of all 32
+    static constexpr int kScales = !E4M3 ? 0 : ROWS == 256 ? kWaves * kWave * 4 : ROWS * 4, kScaleSlots = 4;
+    static constexpr int kScalesAt = kRing > kEmit ? kRing : kEmit;
+    static constexpr int kLds = kScalesAt + kScaleSlots * kScales;
+    static constexpr int kOutput = GATED ? HALF : 2 * HALF;          // output features of a tile
     using Acc = v4f;
     using Frag = typename std::conditional<E4M3, v8i, v8bf>::type;
     enum Unit { A0, A1, B0, B1 };
@@ -207,30 +213,43 @@ struct Tile {
         asm volatile("" : "+v"(tid));
         int lane = tid & (kWave - 1);
         const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
-        const int wf = wave & 1, wr = wave >> 1;
+        const int wf = wave % kWavesF, wr = wave / kWavesF;
         const int size = E4M3 ? 1 : 2;
         const int k = FORM == kWeightGradient ? rows.n : P.k;          // contraction
         const int n_b = FORM == kWeightGradient ? P.other : rows.n;    // rows of operand b
         const int steps = (int)(((long long)k * size + kStep - 1) / kStep);
+        // Few rows: one unit of B.  The weights are then read once and their reading is what takes time, and where rows are
+        // a power of two apart one step's loads all fall on a few memory channels.  So workgroups begin at different steps and
+        // wrap round: 128 experts of 2 x 768 x 2048 at 16 rows 196 -> 153 us.  (With more rows it would part the
+        // workgroups that share operands: 487 -> 499 us.)
+        const bool few = kHalves == 1 || n_b - r0 <= kUnitRows;
+        const int shift = (int)((long long)blockIdx.x * steps / gridDim.x);
+        using Turned = std::integral_constant<bool, true>;
+        using Straight = std::integral_constant<bool, false>;
+        auto place_of = [&](int step, auto turn) {
+            if constexpr (turn()) return step + shift < steps ? step + shift : step + shift - steps;
+            else return step;
+        };
 
         // Where this lane's chunks come from.  Past the end of the features there are others that are as good (what is
         // computed from them is not written); past the rows and past the contraction there are zeros.
-        unsigned off[2][4];                        // [operand][two loads of each unit]
+        unsigned off[2][4];                        // [operand][loads of both units]
         int steps_here[2];                         // steps in which this lane's chunk of a load is there (transposed: of both)
-        const int chunk = (lane & 7) ^ swizzle(wave * 8 + (lane >> 3));           // as lies, contiguous along the contraction
         const int depth = wave * 4 + (lane >> 4), column = ((lane & 15) ^ spread(depth)) * 8;       // transposed
 #pragma unroll
         for (int o = 0; o < 2; ++o) {
             const bool trans = o ? kTransB : kTransA;
             const int ld = o ? P.b_ld : P.a_ld, end = o ? n_b - r0 : P.features - f0;
+            const int load_rows = o ? kLoadRowsB : 8;  // contiguous along the contraction
+            const int chunk = (lane & 7) ^ swizzle(wave * load_rows + (lane >> 3));
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
+            for (int j = 0; j < (o ? kHalves * kLoadsB : 4); ++j) {
                 if (trans) {
-                    const int f = (j >> 1) * kHalf + column;
+                    const int f = (j >> 1) * HALF + column;
                     off[o][j] = (unsigned)(depth + (j & 1) * 32) * ld + (f < end ? f : 0) * 2;
                 } else {
-                    int r = (j * kWaves + wave) * 8 + (lane >> 3);
-                    if (!o && GATED) r &= kHalf - 1;
+                    int r = (j * kWaves + wave) * load_rows + (lane >> 3);
+                    if (!o && GATED) r &= HALF - 1;
                     off[o][j] = r < end ? (unsigned)r * ld + chunk * 16 : o ? kNowhere : (unsigned)chunk * 16;
                 }
             }
@@ -249,35 +268,47 @@ struct Tile {
         const int per_row = P.k / 128;
         if (E4M3) {                                                    // scales: of a row and of 128 features, one a step
             const int blocks = (P.features + 127) / 128;
-            const Constant first = (Constant)(uintptr_t)P.a_scales + (size_t)e * blocks * (GATED ? 2 : 1) * per_row + (size_t)(f0 / 128) * per_row;
-            sa[0] = first;
-            sa[1] = GATED ? first + (size_t)blocks * per_row : f0 / 128 + 1 < blocks ? first + per_row : first;
+            const Constant first = (Constant)(uintptr_t)P.a_scales + (size_t)e * blocks * (GATED ? 2 : 1) * per_row;
+            const int block = f0 / 128, second = (f0 + HALF) / 128;
+            sa[0] = first + (size_t)block * per_row;
+            sa[1] = first + (size_t)(GATED ? blocks + block : second < blocks ? second : block) * per_row;
             sb = (const char *)(P.b_scales + (size_t)(rows.first + r0) * per_row);
-            int r = (lane >> 5) * kHalf + wr * 32 + (lane & 31);       // lane: B0's rows of this wave, then B1's
+            // 256 rows: this wave's in B0, then in B1; 32 rows: each wave a share of them
+            int r = ROWS == 256 ? (lane >> 5) * kUnitRows + wr * 32 + (lane & 31) : wave * kLoadRowsB + (lane & (kLoadRowsB - 1));
             if (r >= n_b - r0) r = 0;
             off_s = (unsigned)r * per_row * 4;
         }
 
         const unsigned lds0 = lds_address(lds);
         // [slot][A0, A1], then [slot][B0, B1]: what one operand's reads span fits their instructions' offset
-        auto place = [](int unit, int slot) constexpr { return unit < B0 ? (slot * 2 + unit) * kUnit : (4 + slot * kHalves + unit - B0) * kUnit; };
-        constexpr int kScalesAt = kRing > kEmit ? kRing : kEmit;
-        auto scales_at = [&](int step) { return kScalesAt + ((step & (kScaleSlots - 1)) * kWaves + wave) * kWave * 4; };
-        auto load = [&](int unit, int step) {
+        auto place = [](int unit, int slot) constexpr {
+            return unit < B0 ? (slot * 2 + unit) * kUnitA : 4 * kUnitA + (slot * kHalves + unit - B0) * kUnitB;
+        };
+        auto scales_at = [](int step, int wave) { return kScalesAt + ((step & (kScaleSlots - 1)) * kScales) + (ROWS == 256 ? wave * kWave * 4 : 0); };
+        auto load = [&](int unit, int step, auto turn) {
             const int o = unit >= B0, u = o ? unit - B0 : unit;
             const bool trans = o ? kTransB : kTransA;
-            const int ld = o ? P.b_ld : P.a_ld;
+            const int ld = o ? P.b_ld : P.a_ld, at_k = place_of(step, turn);
             const char *base = o ? b0 : u ? a1 : a0;
-            const Window from(trans ? base + (size_t)step * 64 * ld : base);
-            const unsigned to = lds0 + place(unit, step & 1) + wave * 1024;
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const bool there = trans && j ? step * 64 + depth + 32 < k : step < steps_here[o];
-                to_lds_16(from, there ? off[o][u * 2 + j] : kNowhere, trans ? 0 : step * kStep, to + j * kWaves * 1024);
+            const Window from(trans ? base + (size_t)at_k * 64 * ld : base);
+            const unsigned to = lds0 + place(unit, step & 1) + wave * (o ? kLoadRowsB * kStep : 1024);
+            auto one = [&](int j) {
+                const bool there = step < steps && (trans && j ? at_k * 64 + depth + 32 < k : at_k < steps_here[o]);
+                to_lds_16(from, there ? off[o][u * 2 + j] : kNowhere, trans ? 0 : at_k * kStep, to + j * kWaves * 1024);
+            };
+            if (o && kLoadRowsB < 8) {
+                if (lane < kLoadRowsB * 8) one(0);
+            } else {
+                one(0);
+                if (!o || kLoadsB == 2) one(1);
             }
         };
-        auto load_scales = [&](int step) {
-            if (E4M3) to_lds_4(Window(sb), step < steps ? off_s : kNowhere, step * 4, lds0 + scales_at(step));
+        auto load_scales = [&](int step, auto turn) {
+            if constexpr (E4M3) {
+                const unsigned from = step < steps ? off_s : kNowhere, shift_by = place_of(step, turn) * 4;
+                if (ROWS == 256) to_lds_4(Window(sb), from, shift_by, lds0 + scales_at(step, wave));
+                else if (lane < kLoadRowsB) to_lds_4(Window(sb), from, shift_by, lds0 + scales_at(step, 0) + wave * kLoadRowsB * 4);
+            }
         };
 
         // This wave's fragments of a unit.  Their places differ from the first one's by constants and, where the swizzle
@@ -290,7 +321,7 @@ struct Tile {
         unsigned at[2][kPatterns];
 #pragma unroll
         for (int o = 0; o < 2; ++o) {
-            const int first = o ? wr * 32 : wf * 64, unit = lds0 + place(o ? B0 : A0, 0);
+            const int first = o ? wr * kOwnR : wf * kOwnF, unit = lds0 + place(o ? B0 : A0, 0);
 #pragma unroll
             for (int p = 0; p < kPatterns; ++p) {
                 if (o ? kTransB : kTransA) {
@@ -341,27 +372,24 @@ struct Tile {
         auto multiply = [&](auto half_a, auto half_b, const Frag (&b)[kFragsR][kParts], float w, auto next) {
             constexpr int h = decltype(half_a)::value, g = decltype(half_b)::value;
             if constexpr (E4M3) {
-                // a block's sum enters the accumulators, times both scales, while the next fragment's is on its way
-                v4f sum[2][kFragsR];
-                auto add = [&](int i) {
+                // a block's sum enters the accumulators, times both scales, while the next one is on its way
+                v4f sum[2];
+                auto add = [&](int n) {
+                    const int i = n / kFragsR, j = n % kFragsR;
+                    const float f = row_scale[j] * w;
 #pragma unroll
-                    for (int j = 0; j < kFragsR; ++j) {
-                        const float f = row_scale[j] * w;
-#pragma unroll
-                        for (int t = 0; t < 4; ++t) acc[h][g][i][j][t] = fmaf(sum[i & 1][j][t], f, acc[h][g][i][j][t]);
-                    }
+                    for (int t = 0; t < 4; ++t) acc[h][g][i][j][t] = fmaf(sum[n & 1][t], f, acc[h][g][i][j][t]);
                 };
 #pragma unroll
-                for (int i = 0; i < kFragsF; ++i) {
+                for (int n = 0; n < kFragsF * kFragsR; ++n) {
+                    const int i = n / kFragsR, j = n % kFragsR;
                     const v4f zero = {0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-                    for (int j = 0; j < kFragsR; ++j)
-                        sum[i & 1][j] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa[i][0], b[j][0], zero, 0, 0, 0, 0, 0, 0);
-                    next(i, 0);
+                    sum[n & 1] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fa[i][0], b[j][0], zero, 0, 0, 0, 0, 0, 0);
+                    if (j == kFragsR - 1) next(i, 0);
                     __builtin_amdgcn_sched_barrier(0);
-                    if (i) add(i - 1);
+                    if (n) add(n - 1);
                 }
-                add(kFragsF - 1);
+                add(kFragsF * kFragsR - 1);
             } else {
 #pragma unroll
                 for (int part = 0; part < kParts; ++part)
@@ -380,16 +408,17 @@ struct Tile {
         auto nothing = [](int, int) {};
         // What one wave does for step `step`; s: step & 1.
         float w[2] = {0.0f, 0.0f};
-        auto scales_of_weights = [&](int step, auto parity) {
+        auto scales_of_weights = [&](int step, auto parity, auto turn) {
             if constexpr (E4M3) {
                 const bool there = !parity() || step < steps;          // behind an odd last step there is one of zeros
-                w[0] = sa[0][there ? step : step - 1]; w[1] = sa[1][there ? step : step - 1];
+                const int at_k = there ? place_of(step, turn) : 0;
+                w[0] = sa[0][at_k]; w[1] = sa[1][at_k];
                 if (!there) w[0] = w[1] = 0.0f;
             }
         };
         auto scales_of = [&](int step, int g) {                        // of the rows of a unit of B
             if constexpr (E4M3) {
-                const float *S = (const float *)(lds + scales_at(step)) + g * 32 + (lane & 15);
+                const float *S = (const float *)(lds + scales_at(step, wave)) + g * 32 + (lane & 15);
 #pragma unroll
                 for (int j = 0; j < kFragsR; ++j) row_scale[j] = S[j * kSide];
             }
@@ -408,60 +437,63 @@ struct Tile {
         };
 
         __syncthreads();                           // the tile before is done with its LDS
-        if (n_b - r0 > kHalf) {
+        if constexpr (kHalves == 2) if (!few) {
             // Loads of this wave that may still be on their way between phases: all but the unit that the next phase reads
             // and those before it, six units of two loads, and in e4m3 a load of scales or two among them.
             constexpr int kAhead = E4M3 ? 13 : 12;
-            load_scales(0); load(B0, 0); load(A0, 0); load(B1, 0); load(A1, 0);
-            load_scales(1); load(B0, 1); load(A0, 1); load(B1, 1); load(A1, 1);
+            Straight t;
+            load_scales(0, t); load(B0, 0, t); load(A0, 0, t); load(B1, 0, t); load(A1, 0, t);
+            load_scales(1, t); load(B0, 1, t); load(A0, 1, t); load(B1, 1, t); load(A1, 1, t);
             loads_done_and_barrier<kAhead>();
             read_a();
             read_b(fb0[0], U_B0(), Zero());
             loads_done_and_barrier<kAhead - 2>();
-            load(B0, 2); load_scales(2); load(A0, 2);
+            load(B0, 2, t); load_scales(2, t); load(A0, 2, t);
             auto body = [&](int step, auto parity) {
                 constexpr int s = parity();
                 using S0 = std::integral_constant<int, s>;
                 using S1 = std::integral_constant<int, 1 - s>;
-                scales_of_weights(step, parity);
+                scales_of_weights(step, parity, t);
                 // 1
                 scales_of(step, 0);
                 read_b(fb1, U_B1(), S0());
                 in_order();
                 multiply(Zero(), Zero(), fb0[s], w[0], nothing);
                 loads_done_and_barrier<kAhead>();
-                load(B1, step + 2);
+                load(B1, step + 2, t);
                 // 2
                 scales_of(step, 1);
                 multiply(Zero(), One(), fb1, w[0], [&](int i, int part) { fa[i][part] = frag(U_A1(), S0(), i, part); });
                 loads_done_and_barrier<kAhead>();
-                load(A1, step + 2);
+                load(A1, step + 2, t);
                 // 3
                 read_b(fb0[1 - s], U_B0(), S1());
                 in_order();
                 multiply(One(), One(), fb1, w[1], nothing);
                 loads_done_and_barrier<kAhead>();
-                load(B0, step + 3);
+                load(B0, step + 3, t);
                 // 4
                 scales_of(step, 0);
                 multiply(One(), Zero(), fb0[s], w[1], [&](int i, int part) { fa[i][part] = frag(U_A0(), S1(), i, part); });
                 loads_done_and_barrier<kAhead>();
-                load_scales(step + 3);
-                load(A0, step + 3);
+                load_scales(step + 3, t);
+                load(A0, step + 3, t);
             };
             for (int step = 0; step < steps; step += 2) {              // behind an odd last step, one of zeros
                 body(step, Zero());
                 body(step + 1, One());
             }
-        } else {
-            // At most 128 rows: no B1, two phases.  Waves whose 32 rows there are none of only load.
-            constexpr int kAhead = E4M3 ? 7 : 6;
-            load_scales(0); load(B0, 0); load(A0, 0); load(A1, 0);
-            load_scales(1); load(B0, 1); load(A0, 1); load(A1, 1);
+        }
+        if (few) {
+            // No B1, two phases.  Waves whose rows there are none of only load.
+            constexpr int kAhead = (E4M3 ? 5 : 4) + kLoadsB;
+            Turned t;
+            load_scales(0, t); load(B0, 0, t); load(A0, 0, t); load(A1, 0, t);
+            load_scales(1, t); load(B0, 1, t); load(A0, 1, t); load(A1, 1, t);
             loads_done_and_barrier<kAhead + 2>();
             auto start = [&] {
                 loads_done_and_barrier<kAhead>();
-                load(B0, 2); load_scales(2); load(A0, 2);
+                load(B0, 2, t); load_scales(2, t); load(A0, 2, t);
             };
             auto body = [&](int step, auto parity, auto present) {
                 constexpr int s = parity();
@@ -469,21 +501,21 @@ struct Tile {
                 using S0 = std::integral_constant<int, s>;
                 using S1 = std::integral_constant<int, 1 - s>;
                 if constexpr (here) {
-                    scales_of_weights(step, parity);
+                    scales_of_weights(step, parity, t);
                     scales_of(step, 0);
                     multiply(Zero(), Zero(), fb0[s], w[0], [&](int i, int part) { fa[i][part] = frag(U_A1(), S0(), i, part); });
                 }
                 loads_done_and_barrier<kAhead>();
-                load(A1, step + 2);
+                load(A1, step + 2, t);
                 if constexpr (here) {
                     read_b(fb0[1 - s], U_B0(), S1());
                     in_order();
                     multiply(One(), Zero(), fb0[s], w[1], [&](int i, int part) { fa[i][part] = frag(U_A0(), S1(), i, part); });
                 }
                 loads_done_and_barrier<kAhead>();
-                load(B0, step + 3); load_scales(step + 3); load(A0, step + 3);
+                load(B0, step + 3, t); load_scales(step + 3, t); load(A0, step + 3, t);
             };
-            if (wr * 32 < n_b - r0) {
+            if (kWavesR == 1 || wr * kOwnR < n_b - r0) {
                 read_a();
                 read_b(fb0[0], U_B0(), Zero());
                 start();
@@ -501,12 +533,13 @@ struct Tile {
         }
         loads_done_and_barrier<0>();               // also those of steps that are none
 
-        // ---- the tile's output, 128 features at a time through LDS, so that rows are written in whole lines
+        // ---- the tile's output, HALF features at a time through LDS, so that rows are written in whole lines
         float *out = (float *)lds;
         tid = threadIdx.x;
         asm volatile("" : "+v"(tid));
         lane = tid & (kWave - 1);
-        const int piece = tid & 15, n_rows = n_b - r0 < ROWS ? n_b - r0 : ROWS;
+        constexpr int kPieces = HALF / 8;                              // of eight features, a lane each
+        const int piece = tid & (kPieces - 1), n_rows = n_b - r0 < ROWS ? n_b - r0 : ROWS;
         // Moves value(g, i, j, t) of a half of the features to LDS and from there, eight features a lane, to put(row, values).
         auto emit = [&](auto value, auto put) {
             __syncthreads();
@@ -516,12 +549,12 @@ struct Tile {
                 for (int i = 0; i < kFragsF; ++i)
 #pragma unroll
                     for (int j = 0; j < kFragsR; ++j) {
-                        const int row = g * kHalf + wr * 32 + j * kSide + (lane & 15), f = wf * 64 + i * kSide + (lane >> 4) * 4;
+                        const int row = g * kUnitRows + wr * kOwnR + j * kSide + (lane & 15), f = wf * kOwnF + i * kSide + (lane >> 4) * 4;
                         const v4f v = {value(g, i, j, 0), value(g, i, j, 1), value(g, i, j, 2), value(g, i, j, 3)};
                         *(v4f *)(out + row * kEmitPitch + f) = v;
                     }
             __syncthreads();
-            for (int row = tid >> 4; row < n_rows; row += kThreads / 16) {
+            for (int row = tid / kPieces; row < n_rows; row += kThreads / kPieces) {
                 const v4f x = *(const v4f *)(out + row * kEmitPitch + piece * 8), y = *(const v4f *)(out + row * kEmitPitch + piece * 8 + 4);
                 const float v[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
                 put(row, v);
@@ -537,7 +570,7 @@ struct Tile {
 #pragma unroll
             for (int i = 0; i < 8; ++i) amax = fabsf(v[i]) > amax ? fabsf(v[i]) : amax;
 #pragma unroll
-            for (int o = 1; o < 16; o <<= 1) amax = fmaxf(amax, __shfl_xor(amax, o));
+            for (int o = 1; o < kPieces; o <<= 1) amax = fmaxf(amax, __shfl_xor(amax, o));
             const float scale = block_scale(amax);
             const v2u w = {e4m3_codes(v, scale), e4m3_codes(v + 4, scale)};
             *(v2u *)((char *)to + row * width + f) = w;
@@ -568,15 +601,17 @@ struct Tile {
             for (int h = 0; h < 2; ++h)
                 emit([&](int g, int i, int j, int t) { return acc[h][g][i][j][t]; },
                      [&](int row, const float *v) {
-                         if (f + h * kHalf < P.features) put_bf16(P.out, row0 + row, f + h * kHalf, P.features, v);
+                         if (f + h * HALF < P.features) put_bf16(P.out, row0 + row, f + h * HALF, P.features, v);
                      });
         }
     }
 };
 
 // Row tiles of the call's experts before each, in LDS: [n + 1].
+template <int THREADS>
 __device__ inline void scan_tiles(const Groups &G, int rows_per_tile, int *before) {
-    __shared__ int part[kThreads / kWave];
+    __shared__ int part[THREADS / kWave];
+    constexpr int kThreads = THREADS, kWaves = THREADS / kWave;
     const int tid = threadIdx.x, lane = tid & (kWave - 1);
     int carry = 0;
     if (tid == 0) before[0] = 0;
@@ -600,22 +635,21 @@ __device__ inline void scan_tiles(const Groups &G, int rows_per_tile, int *befor
     }
 }
 
-constexpr int kXcds = 8;
 constexpr int kRowGroup = 8;                   // row tiles that walk the features together
 
-template <int FORM, bool E4M3, bool GATED, int ROWS>
-__global__ __launch_bounds__(kThreads) void expert_tiles_kernel(Groups G, Product P) {
-    using T = Tile<FORM, E4M3, GATED, ROWS>;
+template <int FORM, bool E4M3, bool GATED, int ROWS, int HALF>
+__global__ __launch_bounds__((Tile<FORM, E4M3, GATED, ROWS, HALF>::kThreads), 2) void expert_tiles_kernel(Groups G, Product P) {
+    using T = Tile<FORM, E4M3, GATED, ROWS, HALF>;
     __shared__ __align__(1024) char lds[T::kLds];
     __shared__ int before[kMaxExperts + 1];
     const int columns = (P.features + T::kOutput - 1) / T::kOutput;
     const int fixed = FORM == kWeightGradient ? (P.other + ROWS - 1) / ROWS : 0;
-    if (FORM != kWeightGradient) scan_tiles(G, ROWS, before);
+    if (FORM != kWeightGradient) scan_tiles<T::kThreads>(G, ROWS, before);
     const long long tiles = (long long)(FORM == kWeightGradient ? G.n * fixed : before[G.n]) * columns;
-    // workgroups go to the XCDs in turn: those of one XCD take neighbouring tiles, whose operands its L2 then holds
-    const int per_xcd = gridDim.x / kXcds;
-    const long long mine = (long long)(blockIdx.x % kXcds) * per_xcd + blockIdx.x / kXcds;
-    for (long long t = mine; t < tiles; t += gridDim.x) {
+    // Workgroups go to the XCDs in turn.  Each XCD has an eighth of the tiles, neighbours, whose operands its L2 then holds.
+    const int xcd = blockIdx.x % kXcds;
+    const long long end = tiles * (xcd + 1) / kXcds;
+    for (long long t = tiles * xcd / kXcds + blockIdx.x / kXcds; t < end; t += gridDim.x / kXcds) {
         const int row_tile = (int)(t / columns);                       // counted over the experts
         int lo = 0, hi = G.n, n_tiles, index;
         if constexpr (FORM == kWeightGradient) {
