@@ -14,7 +14,6 @@ namespace flmoe {
 namespace experts {
 
 constexpr int kMaxWidth = 1 << 20;             // as fl_moe_config.hidden
-constexpr long long kFewRows = 32;             // see launch_tiles
 constexpr int kUnits = 256;                    // compute units of the part
 
 // What a call's configuration and tables come to.
@@ -64,29 +63,37 @@ inline int compute_units() {
 inline int launched() { return hipGetLastError() == hipSuccess ? FL_OK : FL_ERR_HIP; }
 
 // mean: rows an expert would have if the tokens of the configuration were spread evenly.
+// Experts of few rows are bound by the reading of their weights; smaller tiles leave less of the machine idle at the beginning
+// and the end of each and spread few experts over more compute units.  us of both products of one call, 128 experts of
+// 2 x 768 x 2048 in bf16, tiles of 256, 64 and 32 rows: 16 rows 156 / 89, 146 / 80 and 143 / 77; 48 rows 160 / 103, 152 / 91;
+// 64 rows 164 / 107, 156 / 94; 128 rows 185 / 126, 217 / 131; e4m3, 64 experts of 7168 x 2048, the product behind, 4 rows 174, 185,
+// 159.  The counts scatter round their mean, so that an expert hardly ever has two tiles where one was meant:
+constexpr long long kRowsFor32 = 20, kRowsFor64 = 48;
+// Workgroups of small tiles on a compute unit: what is on its way to one is best 64 to 96 KB (32 KB each); the third pays where a
+// tile is short (128 experts, e4m3, 768 long: 44 -> 36 us, bf16 2048 long 143 -> 147).
+constexpr int kShortBytes = 2048;
+
 template <int FORM, bool E4M3, bool GATED>
 int launch_tiles(const Groups &G, long long mean, const Product &P, hipStream_t st) {
+    using std::integral_constant;
     const int units = std::max(1, compute_units() / kXcds) * kXcds;
     auto go = [&](auto rows, auto half, int per_unit) {
         using T = Tile<FORM, E4M3, GATED, rows(), half()>;
         expert_tiles_kernel<FORM, E4M3, GATED, rows(), half()><<<dim3(units * per_unit), dim3(T::kThreads), 0, st>>>(G, P);
+        return launched();
     };
-    using std::integral_constant;
     if constexpr (FORM == kForward) {
-        if (mean <= kFewRows) {
-            // (what answers in blocks of 128 features has to have them in one tile)
-            if constexpr (GATED) {
-                if (E4M3 || P.pre_scales) {
-                    go(integral_constant<int, 32>(), integral_constant<int, 128>(), 1);
-                    return launched();
-                }
-            }
-            if constexpr (!(E4M3 && GATED)) go(integral_constant<int, 32>(), integral_constant<int, 64>(), P.k * (E4M3 ? 1 : 2) <= 2048 ? 3 : 2);
-            return launched();
+        if constexpr (GATED) {                     // what answers in blocks of 128 features has them in one tile
+            if (mean <= kRowsFor64 && (E4M3 || P.pre_scales))
+                return go(integral_constant<int, 64>(), integral_constant<int, 128>(), 1);
+        }
+        if constexpr (!(E4M3 && GATED)) {
+            const int per_unit = P.k * (E4M3 ? 1 : 2) <= kShortBytes ? 3 : 2;
+            if (mean <= kRowsFor32) return go(integral_constant<int, 32>(), integral_constant<int, 64>(), per_unit);
+            if (mean <= kRowsFor64) return go(integral_constant<int, 64>(), integral_constant<int, 64>(), per_unit);
         }
     }
-    go(integral_constant<int, 256>(), integral_constant<int, 128>(), 1);
-    return launched();
+    return go(integral_constant<int, 256>(), integral_constant<int, 128>(), 1);
 }
 
 // y = x W^T, W [experts][out][in]

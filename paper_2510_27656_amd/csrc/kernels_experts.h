@@ -104,6 +104,8 @@ __device__ inline unsigned e4m3_codes(const float *v, float scale) {
 }
 
 // ---------------------------------------------------------------- memory
+// (Lambdas that hold fragments or accumulators by reference: called instead of inlined they would put them into memory.)
+#define FLMOE_INLINE __attribute__((always_inline))
 // A lane's 16 (or 4) bytes straight into LDS, at the wave's place there plus 16 (4) times the lane.  Offsets of kNowhere
 // read as zero; only offsets inside the tensor or kNowhere are ever passed, the limit is the largest there is.  Written
 // out because the compiler, which knows that these loads write LDS, lets every read of LDS behind them wait for them:
@@ -178,11 +180,11 @@ struct Product {
 __device__ inline int swizzle(int row) { return row >> 1 & 7; }
 __device__ inline int spread(int row) { return (row & 3) << 2 | (row >> 2 & 2); }
 
-// ROWS: 256, or 32 for experts of few rows, with HALF features to a unit of A (a wave for every 16 of them).
+// ROWS: 256; or for experts of few rows 64 or 32, with HALF features to a unit of A, a wave for every 16 of them.
 template <int FORM, bool E4M3, bool GATED, int ROWS, int HALF>
 struct Tile {
     static constexpr bool kTransA = FORM != kForward, kTransB = FORM == kWeightGradient;
-    static_assert((ROWS == 256 && HALF == 128) || (ROWS == 32 && FORM == kForward && (HALF == 128 || HALF == 64)), "");
+    static_assert((ROWS == 256 && HALF == 128) || (FORM == kForward && ((ROWS == 64 && HALF == 128) || (ROWS <= 64 && HALF == 64))), "");
     static constexpr int kThreads = ROWS == 256 ? 512 : HALF * 4, kWaves = kThreads / kWave;
     // Matrix instructions of 16 by 16 outputs, 64 bytes of bf16 or 128 of e4m3 deep.  (Alone on the machine they reach
     // 2370 Tflop/s in bf16, 1930 with random operands; those of 32 by 32 outputs 1600 and 1310.)
@@ -192,12 +194,11 @@ struct Tile {
     static constexpr int kWavesF = ROWS == 256 ? 2 : kWaves, kWavesR = kWaves / kWavesF;
     static constexpr int kOwnF = HALF / kWavesF, kOwnR = kUnitRows / kWavesR;         // of a wave in a unit
     static constexpr int kFragsF = kOwnF / kSide, kFragsR = kOwnR / kSide;
-    static constexpr int kLoadsB = ROWS == 256 ? 2 : 1;                // of a wave for a unit of B
-    static constexpr int kLoadRowsB = kUnitRows / kWaves / kLoadsB;    // ... of 8 rows each, or of 4 by half the lanes
+    static constexpr int kLoadsB = kUnitRows / kWaves / 8;             // of a wave for a unit of B
     static constexpr int kRing = 4 * kUnitA + 2 * kHalves * kUnitB;    // [two][A0, A1], [two][B0, B1]
     static constexpr int kEmitPitch = HALF + 4;                        // floats from row to row of the output in LDS
     static constexpr int kEmit = ROWS * kEmitPitch * 4;
-    // scales of the rows of a step: those of its own rows for each wave, or of all 32
+    // scales of the rows of a step: those of its own rows for each wave, or of all
     static constexpr int kScales = !E4M3 ? 0 : ROWS == 256 ? kWaves * kWave * 4 : ROWS * 4, kScaleSlots = 4;
     static constexpr int kScalesAt = kRing > kEmit ? kRing : kEmit;
     static constexpr int kLds = kScalesAt + kScaleSlots * kScales;
@@ -240,15 +241,14 @@ struct Tile {
         for (int o = 0; o < 2; ++o) {
             const bool trans = o ? kTransB : kTransA;
             const int ld = o ? P.b_ld : P.a_ld, end = o ? n_b - r0 : P.features - f0;
-            const int load_rows = o ? kLoadRowsB : 8;  // contiguous along the contraction
-            const int chunk = (lane & 7) ^ swizzle(wave * load_rows + (lane >> 3));
+            const int chunk = (lane & 7) ^ swizzle(wave * 8 + (lane >> 3));             // contiguous along the contraction
 #pragma unroll
             for (int j = 0; j < (o ? kHalves * kLoadsB : 4); ++j) {
                 if (trans) {
                     const int f = (j >> 1) * HALF + column;
                     off[o][j] = (unsigned)(depth + (j & 1) * 32) * ld + (f < end ? f : 0) * 2;
                 } else {
-                    int r = (j * kWaves + wave) * load_rows + (lane >> 3);
+                    int r = (j * kWaves + wave) * 8 + (lane >> 3);
                     if (!o && GATED) r &= HALF - 1;
                     off[o][j] = r < end ? (unsigned)r * ld + chunk * 16 : o ? kNowhere : (unsigned)chunk * 16;
                 }
@@ -273,8 +273,8 @@ struct Tile {
             sa[0] = first + (size_t)block * per_row;
             sa[1] = first + (size_t)(GATED ? blocks + block : second < blocks ? second : block) * per_row;
             sb = (const char *)(P.b_scales + (size_t)(rows.first + r0) * per_row);
-            // 256 rows: this wave's in B0, then in B1; 32 rows: each wave a share of them
-            int r = ROWS == 256 ? (lane >> 5) * kUnitRows + wr * 32 + (lane & 31) : wave * kLoadRowsB + (lane & (kLoadRowsB - 1));
+            // this wave's in B0, then in B1; of 64 rows each wave a share
+            int r = ROWS == 256 ? (lane >> 5) * kUnitRows + wr * 32 + (lane & 31) : wave * kLoadsB * 8 + (lane & (kLoadsB * 8 - 1));
             if (r >= n_b - r0) r = 0;
             off_s = (unsigned)r * per_row * 4;
         }
@@ -285,29 +285,25 @@ struct Tile {
             return unit < B0 ? (slot * 2 + unit) * kUnitA : 4 * kUnitA + (slot * kHalves + unit - B0) * kUnitB;
         };
         auto scales_at = [](int step, int wave) { return kScalesAt + ((step & (kScaleSlots - 1)) * kScales) + (ROWS == 256 ? wave * kWave * 4 : 0); };
-        auto load = [&](int unit, int step, auto turn) {
+        auto load = [&](int unit, int step, auto turn) FLMOE_INLINE {
             const int o = unit >= B0, u = o ? unit - B0 : unit;
             const bool trans = o ? kTransB : kTransA;
             const int ld = o ? P.b_ld : P.a_ld, at_k = place_of(step, turn);
             const char *base = o ? b0 : u ? a1 : a0;
             const Window from(trans ? base + (size_t)at_k * 64 * ld : base);
-            const unsigned to = lds0 + place(unit, step & 1) + wave * (o ? kLoadRowsB * kStep : 1024);
+            const unsigned to = lds0 + place(unit, step & 1) + wave * 1024;
             auto one = [&](int j) {
                 const bool there = step < steps && (trans && j ? at_k * 64 + depth + 32 < k : at_k < steps_here[o]);
                 to_lds_16(from, there ? off[o][u * 2 + j] : kNowhere, trans ? 0 : at_k * kStep, to + j * kWaves * 1024);
             };
-            if (o && kLoadRowsB < 8) {
-                if (lane < kLoadRowsB * 8) one(0);
-            } else {
-                one(0);
-                if (!o || kLoadsB == 2) one(1);
-            }
+            one(0);
+            if (!o || kLoadsB == 2) one(1);
         };
         auto load_scales = [&](int step, auto turn) {
             if constexpr (E4M3) {
                 const unsigned from = step < steps ? off_s : kNowhere, shift_by = place_of(step, turn) * 4;
                 if (ROWS == 256) to_lds_4(Window(sb), from, shift_by, lds0 + scales_at(step, wave));
-                else if (lane < kLoadRowsB) to_lds_4(Window(sb), from, shift_by, lds0 + scales_at(step, 0) + wave * kLoadRowsB * 4);
+                else if (lane < kLoadsB * 8) to_lds_4(Window(sb), from, shift_by, lds0 + scales_at(step, 0) + wave * kLoadsB * 32);
             }
         };
 
@@ -334,8 +330,9 @@ struct Tile {
                 asm volatile("" : "+v"(at[o][p]));                     // not to be worked out again at every use
             }
         }
-        auto frag = [&](auto unit, auto slot, int i, int part) -> Frag {
-            constexpr int o = unit() >= B0, base = place(unit(), slot()) - place(o ? B0 : A0, 0);
+        // base: from the operand's first unit to the fragment's
+        auto frag = [&](auto operand, int base, int i, int part) FLMOE_INLINE -> Frag {
+            constexpr int o = operand();
             if constexpr (E4M3) {
                 const v4i lo = *(FLMOE_LDS const v4i *)(uintptr_t)(at[o][0] + base + i * kSide * kStep);
                 const v4i hi = *(FLMOE_LDS const v4i *)(uintptr_t)(at[o][1] + base + i * kSide * kStep);
@@ -349,11 +346,6 @@ struct Tile {
                 return *(FLMOE_LDS const v8bf *)(uintptr_t)(at[o][part] + base + i * kSide * kStep);
             }
         };
-        using U_A0 = std::integral_constant<int, A0>;
-        using U_A1 = std::integral_constant<int, A1>;
-        using U_B0 = std::integral_constant<int, B0>;
-        using U_B1 = std::integral_constant<int, B1>;
-
         Acc acc[2][kHalves][kFragsF][kFragsR];
 #pragma unroll
         for (int h = 0; h < 2; ++h)
@@ -369,7 +361,7 @@ struct Tile {
         Frag fa[kFragsF][kParts], fb0[2][kFragsR][kParts], fb1[kFragsR][kParts];
         float row_scale[kFragsR];
         // multiplies the fragments at hand into quadrant (h, g); next(i, part) follows a fragment's last use
-        auto multiply = [&](auto half_a, auto half_b, const Frag (&b)[kFragsR][kParts], float w, auto next) {
+        auto multiply = [&](auto half_a, auto half_b, const Frag (&b)[kFragsR][kParts], float w, auto next) FLMOE_INLINE {
             constexpr int h = decltype(half_a)::value, g = decltype(half_b)::value;
             if constexpr (E4M3) {
                 // a block's sum enters the accumulators, times both scales, while the next one is on its way
@@ -423,58 +415,64 @@ struct Tile {
                 for (int j = 0; j < kFragsR; ++j) row_scale[j] = S[j * kSide];
             }
         };
-        auto read_b = [&](Frag (&to)[kFragsR][kParts], auto unit, auto slot) {
+        auto read_b = [&](Frag (&to)[kFragsR][kParts], int base) FLMOE_INLINE {
 #pragma unroll
             for (int part = 0; part < kParts; ++part)
 #pragma unroll
-                for (int j = 0; j < kFragsR; ++j) to[j][part] = frag(unit, slot, j, part);
+                for (int j = 0; j < kFragsR; ++j) to[j][part] = frag(One(), base, j, part);
         };
-        auto read_a = [&] {
+        auto read_a = [&](int base) FLMOE_INLINE {
 #pragma unroll
             for (int part = 0; part < kParts; ++part)
 #pragma unroll
-                for (int i = 0; i < kFragsF; ++i) fa[i][part] = frag(U_A0(), Zero(), i, part);
+                for (int i = 0; i < kFragsF; ++i) fa[i][part] = frag(Zero(), base, i, part);
+        };
+        // multiplies while the next fragments of A are read over the present ones
+        auto multiply_and_read_a = [&](auto half_a, auto half_b, const Frag (&b)[kFragsR][kParts], float w, int base) FLMOE_INLINE {
+            multiply(half_a, half_b, b, w, [&](int i, int part) FLMOE_INLINE { fa[i][part] = frag(Zero(), base, i, part); });
         };
 
         __syncthreads();                           // the tile before is done with its LDS
-        if constexpr (kHalves == 2) if (!few) {
+        auto two_units = [&]() FLMOE_INLINE {
             // Loads of this wave that may still be on their way between phases: all but the unit that the next phase reads
             // and those before it, six units of two loads, and in e4m3 a load of scales or two among them.
             constexpr int kAhead = E4M3 ? 13 : 12;
             Straight t;
-            load_scales(0, t); load(B0, 0, t); load(A0, 0, t); load(B1, 0, t); load(A1, 0, t);
-            load_scales(1, t); load(B0, 1, t); load(A0, 1, t); load(B1, 1, t); load(A1, 1, t);
+#pragma unroll
+            for (int step = 0; step < 2; ++step) {
+                load_scales(step, t);
+                load(B0, step, t); load(A0, step, t); load(B1, step, t); load(A1, step, t);
+            }
             loads_done_and_barrier<kAhead>();
-            read_a();
-            read_b(fb0[0], U_B0(), Zero());
+            read_a(0);
+            read_b(fb0[0], 0);
             loads_done_and_barrier<kAhead - 2>();
             load(B0, 2, t); load_scales(2, t); load(A0, 2, t);
-            auto body = [&](int step, auto parity) {
+            auto body = [&](int step, auto parity) FLMOE_INLINE {
                 constexpr int s = parity();
-                using S0 = std::integral_constant<int, s>;
-                using S1 = std::integral_constant<int, 1 - s>;
+                constexpr int a_here = s * 2 * kUnitA, a_next = (1 - s) * 2 * kUnitA, b_here = s * kHalves * kUnitB, b_next = (1 - s) * kHalves * kUnitB;
                 scales_of_weights(step, parity, t);
                 // 1
                 scales_of(step, 0);
-                read_b(fb1, U_B1(), S0());
+                read_b(fb1, b_here + kUnitB);
                 in_order();
                 multiply(Zero(), Zero(), fb0[s], w[0], nothing);
                 loads_done_and_barrier<kAhead>();
                 load(B1, step + 2, t);
                 // 2
                 scales_of(step, 1);
-                multiply(Zero(), One(), fb1, w[0], [&](int i, int part) { fa[i][part] = frag(U_A1(), S0(), i, part); });
+                multiply_and_read_a(Zero(), One(), fb1, w[0], a_here + kUnitA);
                 loads_done_and_barrier<kAhead>();
                 load(A1, step + 2, t);
                 // 3
-                read_b(fb0[1 - s], U_B0(), S1());
+                read_b(fb0[1 - s], b_next);
                 in_order();
                 multiply(One(), One(), fb1, w[1], nothing);
                 loads_done_and_barrier<kAhead>();
                 load(B0, step + 3, t);
                 // 4
                 scales_of(step, 0);
-                multiply(One(), Zero(), fb0[s], w[1], [&](int i, int part) { fa[i][part] = frag(U_A0(), S1(), i, part); });
+                multiply_and_read_a(One(), Zero(), fb0[s], w[1], a_next);
                 loads_done_and_barrier<kAhead>();
                 load_scales(step + 3, t);
                 load(A0, step + 3, t);
@@ -483,54 +481,59 @@ struct Tile {
                 body(step, Zero());
                 body(step + 1, One());
             }
-        }
-        if (few) {
-            // No B1, two phases.  Waves whose rows there are none of only load.
-            constexpr int kAhead = (E4M3 ? 5 : 4) + kLoadsB;
+        };
+        auto one_unit = [&]() FLMOE_INLINE {
+            // No B1, two phases: A0 B0 while A1 is read over A0, then A1 B0 while the next step's A0 and B0 are read.  Waves
+            // whose rows there are none of only load.
+            constexpr int kAhead = 4 + kLoadsB + (E4M3 ? 1 : 0);
             Turned t;
-            load_scales(0, t); load(B0, 0, t); load(A0, 0, t); load(A1, 0, t);
-            load_scales(1, t); load(B0, 1, t); load(A0, 1, t); load(A1, 1, t);
+#pragma unroll
+            for (int step = 0; step < 2; ++step) {
+                load(B0, step, t); load_scales(step, t); load(A0, step, t); load(A1, step, t);
+            }
             loads_done_and_barrier<kAhead + 2>();
-            auto start = [&] {
+            auto start = [&]() FLMOE_INLINE {
                 loads_done_and_barrier<kAhead>();
                 load(B0, 2, t); load_scales(2, t); load(A0, 2, t);
             };
-            auto body = [&](int step, auto parity, auto present) {
+            auto body = [&](int step, auto parity, auto present) FLMOE_INLINE {
                 constexpr int s = parity();
                 constexpr bool here = present();
-                using S0 = std::integral_constant<int, s>;
-                using S1 = std::integral_constant<int, 1 - s>;
+                constexpr int a_here = s * 2 * kUnitA, a_next = (1 - s) * 2 * kUnitA, b_next = (1 - s) * kHalves * kUnitB;
                 if constexpr (here) {
                     scales_of_weights(step, parity, t);
                     scales_of(step, 0);
-                    multiply(Zero(), Zero(), fb0[s], w[0], [&](int i, int part) { fa[i][part] = frag(U_A1(), S0(), i, part); });
+                    multiply_and_read_a(Zero(), Zero(), fb0[s], w[0], a_here + kUnitA);
                 }
                 loads_done_and_barrier<kAhead>();
                 load(A1, step + 2, t);
                 if constexpr (here) {
-                    read_b(fb0[1 - s], U_B0(), S1());
+                    read_b(fb0[1 - s], b_next);
                     in_order();
-                    multiply(One(), Zero(), fb0[s], w[1], [&](int i, int part) { fa[i][part] = frag(U_A0(), S1(), i, part); });
+                    multiply_and_read_a(One(), Zero(), fb0[s], w[1], a_next);
                 }
                 loads_done_and_barrier<kAhead>();
                 load(B0, step + 3, t); load_scales(step + 3, t); load(A0, step + 3, t);
             };
-            if (kWavesR == 1 || wr * kOwnR < n_b - r0) {
-                read_a();
-                read_b(fb0[0], U_B0(), Zero());
-                start();
-                for (int step = 0; step < steps; step += 2) {
-                    body(step, Zero(), One());
-                    body(step + 1, One(), One());
+            auto all = [&](auto present) FLMOE_INLINE {
+                for (int step = 0; step < steps; step += 2) {          // behind an odd last step, one of zeros
+                    body(step, Zero(), present);
+                    body(step + 1, One(), present);
                 }
+            };
+            if (kWavesR == 1 || wr * kOwnR < n_b - r0) {
+                read_a(0);
+                read_b(fb0[0], 0);
+                start();
+                all(One());
             } else {
                 start();
-                for (int step = 0; step < steps; step += 2) {
-                    body(step, Zero(), Zero());
-                    body(step + 1, One(), Zero());
-                }
+                all(Zero());
             }
-        }
+        };
+        if constexpr (kHalves == 1) one_unit();
+        else if (few) one_unit();
+        else two_units();
         loads_done_and_barrier<0>();               // also those of steps that are none
 
         // ---- the tile's output, HALF features at a time through LDS, so that rows are written in whole lines
@@ -541,7 +544,7 @@ struct Tile {
         constexpr int kPieces = HALF / 8;                              // of eight features, a lane each
         const int piece = tid & (kPieces - 1), n_rows = n_b - r0 < ROWS ? n_b - r0 : ROWS;
         // Moves value(g, i, j, t) of a half of the features to LDS and from there, eight features a lane, to put(row, values).
-        auto emit = [&](auto value, auto put) {
+        auto emit = [&](auto value, auto put) FLMOE_INLINE {
             __syncthreads();
 #pragma unroll
             for (int g = 0; g < kHalves; ++g)
