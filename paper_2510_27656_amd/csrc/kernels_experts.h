@@ -433,49 +433,41 @@ struct Tile {
         };
 
         __syncthreads();                           // the tile before is done with its LDS
-        auto two_units = [&]() FLMOE_INLINE {
-            // Loads of this wave that may still be on their way between phases: all but the unit that the next phase reads
-            // and those before it, six units of two loads, and in e4m3 a load of scales or two among them.
-            constexpr int kAhead = E4M3 ? 13 : 12;
+        auto two_units = [&](auto one) FLMOE_INLINE {                  // (a template, so that it is made where it is called only)
+            using One = decltype(one);
+            // Loads of this wave that may still be on their way between phases: all but the units that the next phase reads
+            // and those before them, four units of two loads, and in e4m3 a load of scales among them.
+            constexpr int kAhead = E4M3 ? 9 : 8;
             Straight t;
 #pragma unroll
             for (int step = 0; step < 2; ++step) {
                 load_scales(step, t);
                 load(B0, step, t); load(A0, step, t); load(B1, step, t); load(A1, step, t);
             }
-            loads_done_and_barrier<kAhead>();
+            loads_done_and_barrier<kAhead + 4>();
             read_a(0);
             read_b(fb0[0], 0);
-            loads_done_and_barrier<kAhead - 2>();
+            loads_done_and_barrier<kAhead>();
             load(B0, 2, t); load_scales(2, t); load(A0, 2, t);
             auto body = [&](int step, auto parity) FLMOE_INLINE {
                 constexpr int s = parity();
-                constexpr int a_here = s * 2 * kUnitA, a_next = (1 - s) * 2 * kUnitA, b_here = s * kHalves * kUnitB, b_next = (1 - s) * kHalves * kUnitB;
+                constexpr int a_here = s * 2 * kUnitA, a_next = (1 - s) * 2 * kUnitA, b_here = s * 2 * kUnitB, b_next = (1 - s) * 2 * kUnitB;
                 scales_of_weights(step, parity, t);
-                // 1
                 scales_of(step, 0);
                 read_b(fb1, b_here + kUnitB);
                 in_order();
                 multiply(Zero(), Zero(), fb0[s], w[0], nothing);
-                loads_done_and_barrier<kAhead>();
-                load(B1, step + 2, t);
-                // 2
                 scales_of(step, 1);
                 multiply_and_read_a(Zero(), One(), fb1, w[0], a_here + kUnitA);
                 loads_done_and_barrier<kAhead>();
-                load(A1, step + 2, t);
-                // 3
+                load(B1, step + 2, t); load(A1, step + 2, t);
                 read_b(fb0[1 - s], b_next);
                 in_order();
                 multiply(One(), One(), fb1, w[1], nothing);
-                loads_done_and_barrier<kAhead>();
-                load(B0, step + 3, t);
-                // 4
                 scales_of(step, 0);
                 multiply_and_read_a(One(), Zero(), fb0[s], w[1], a_next);
                 loads_done_and_barrier<kAhead>();
-                load_scales(step + 3, t);
-                load(A0, step + 3, t);
+                load(B0, step + 3, t); load_scales(step + 3, t); load(A0, step + 3, t);
             };
             for (int step = 0; step < steps; step += 2) {              // behind an odd last step, one of zeros
                 body(step, Zero());
@@ -533,7 +525,7 @@ struct Tile {
         };
         if constexpr (kHalves == 1) one_unit();
         else if (few) one_unit();
-        else two_units();
+        else two_units(One());
         loads_done_and_barrier<0>();               // also those of steps that are none
 
         // ---- the tile's output, HALF features at a time through LDS, so that rows are written in whole lines
