@@ -60,12 +60,10 @@ __device__ inline long long same_in_wave(long long v) {
 
 // ---------------------------------------------------------------- numbers
 __device__ inline float from_bf16(unsigned bits) { return __uint_as_float(bits << 16); }
-__device__ inline unsigned to_bf16(float f) {
-    unsigned u = __float_as_uint(f);
-    if ((u & 0x7fffffffu) > 0x7f800000u) return (u >> 16) | 0x40u;      // NaN stays a quiet NaN
-    return (u + 0x7fffu + ((u >> 16) & 1u)) >> 16;                      // ties to even
+__device__ inline unsigned to_bf16x2(float lo, float hi) {              // to nearest even, NaN stays a quiet NaN
+    typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(unsigned, v2bf{(__bf16)lo, (__bf16)hi});
 }
-__device__ inline unsigned to_bf16x2(float lo, float hi) { return to_bf16(lo) | to_bf16(hi) << 16; }
 
 // silu(v) = v s, s = 1 / (1 + e^-v); gelu(v) = v s with s = 1 / (1 + e^(-2 a (v + 0.044715 v^3))), a = sqrt(2 / pi), which
 // is the tanh form.  *slope receives the derivative; where s has reached 0 or 1 its own derivative is 0, whatever v.
@@ -73,7 +71,7 @@ constexpr float kGelu = 1.5957691216057308f;                            // 2 sqr
 template <bool SLOPE>
 __device__ inline float activate(int act, float v, float *slope) {
     const float arg = act == FL_ACT_SILU ? v : kGelu * (v + 0.044715f * v * v * v);
-    const float s = 1.0f / (1.0f + __expf(-arg));
+    const float s = __builtin_amdgcn_rcpf(1.0f + __expf(-arg));
     if (SLOPE) {
         const float ds = s * (1.0f - s), inner = act == FL_ACT_SILU ? v : kGelu * (v + 3.0f * 0.044715f * v * v * v);
         *slope = ds == 0.0f ? s : s + inner * ds;
@@ -196,35 +194,43 @@ struct Tile {
     static constexpr int kFragsF = kOwnF / kSide, kFragsR = kOwnR / kSide;
     static constexpr int kLoadsB = kUnitRows / kWaves / 8;             // of a wave for a unit of B
     static constexpr int kRing = 4 * kUnitA + 2 * kHalves * kUnitB;    // [two][A0, A1], [two][B0, B1]
-    static constexpr int kEmitPitch = HALF + 4;                        // floats from row to row of the output in LDS
-    static constexpr int kEmit = ROWS * kEmitPitch * 4;
     // scales of the rows of a step: those of its own rows for each wave, or of all
     static constexpr int kScales = !E4M3 ? 0 : ROWS == 256 ? kWaves * kWave * 4 : ROWS * 4, kScaleSlots = 4;
-    static constexpr int kScalesAt = kRing > kEmit ? kRing : kEmit;
-    static constexpr int kLds = kScalesAt + kScaleSlots * kScales;
+    static constexpr int kScalesAt = kRing, kScalesEnd = kScalesAt + kScaleSlots * kScales;
+    // The output passes through LDS: a wave's 64 lanes write eight features each of kEmitRows rows at a time.  In blocks of
+    // e4m3 the largest values of a row in each wave's features pass through it as well.
+    static constexpr int kPieces = kOwnF / 8, kEmitRows = kWave / kPieces, kEmitPitch = kOwnF + 4;
+    static constexpr int kEmit = kWaves * kEmitRows * kEmitPitch * 4;
+    // Tiles of 256 rows have it apart from the ring: the next tile's first loads are on their way meanwhile.
+    static constexpr bool kEarly = ROWS == 256;
+    static constexpr int kEmitAt = kEarly ? kScalesEnd : 0, kLargestAt = kEmitAt + kEmit;
+    static constexpr int kEmitEnd = kLargestAt + (GATED ? kWavesF * ROWS * 4 : 0);
+    static constexpr int kLds = kEmitEnd > kScalesEnd ? kEmitEnd : kScalesEnd;
     static constexpr int kOutput = GATED ? HALF : 2 * HALF;          // output features of a tile
     using Acc = v4f;
     using Frag = typename std::conditional<E4M3, v8i, v8bf>::type;
     enum Unit { A0, A1, B0, B1 };
+    struct Place {
+        int e;                                     // expert
+        Rows rows;                                 // its rows
+        int f0, r0;                                // first output feature; first row (weight gradient: first column of b)
+    };
 
-    // e: expert; rows: its rows; f0: first output feature; r0: first row (weight gradient: first column of b).
-    __device__ static void run(const Product &P, char *lds, int e, const Rows &rows, int f0, int r0) {
-        // (opaque, so that what follows from it is worked out here and not kept in registers from tile to tile)
-        int tid = threadIdx.x;
-        asm volatile("" : "+v"(tid));
-        int lane = tid & (kWave - 1);
+    // next(place): the workgroup's next tile, if there is one.
+    template <class Next>
+    __device__ static void run(const Product &P, char *lds, Next next_place) {
+        const int tid = threadIdx.x, lane = tid & (kWave - 1);
         const int wave = __builtin_amdgcn_readfirstlane(tid / kWave);
         const int wf = wave % kWavesF, wr = wave / kWavesF;
         const int size = E4M3 ? 1 : 2;
-        const int k = FORM == kWeightGradient ? rows.n : P.k;          // contraction
-        const int n_b = FORM == kWeightGradient ? P.other : rows.n;    // rows of operand b
-        const int steps = (int)(((long long)k * size + kStep - 1) / kStep);
+        Place tile;
+        int k, n_b, steps;                         // contraction; rows of operand b; steps
         // Few rows: one unit of B.  The weights are then read once and their reading is what takes time, and where rows are
         // a power of two apart one step's loads all fall on a few memory channels.  So workgroups begin at different steps and
         // wrap round: 128 experts of 2 x 768 x 2048 at 16 rows 196 -> 153 us.  (With more rows it would part the
         // workgroups that share operands: 487 -> 499 us.)
-        const bool few = kHalves == 1 || n_b - r0 <= kUnitRows;
-        const int shift = (int)((long long)blockIdx.x * steps / gridDim.x);
+        bool few;
+        int shift;
         using Turned = std::integral_constant<bool, true>;
         using Straight = std::integral_constant<bool, false>;
         auto place_of = [&](int step, auto turn) {
@@ -236,48 +242,62 @@ struct Tile {
         // computed from them is not written); past the rows and past the contraction there are zeros.
         unsigned off[2][4];                        // [operand][loads of both units]
         int steps_here[2];                         // steps in which this lane's chunk of a load is there (transposed: of both)
-        const int depth = wave * 4 + (lane >> 4), column = ((lane & 15) ^ spread(depth)) * 8;       // transposed
-#pragma unroll
-        for (int o = 0; o < 2; ++o) {
-            const bool trans = o ? kTransB : kTransA;
-            const int ld = o ? P.b_ld : P.a_ld, end = o ? n_b - r0 : P.features - f0;
-            const int chunk = (lane & 7) ^ swizzle(wave * 8 + (lane >> 3));             // contiguous along the contraction
-#pragma unroll
-            for (int j = 0; j < (o ? kHalves * kLoadsB : 4); ++j) {
-                if (trans) {
-                    const int f = (j >> 1) * HALF + column;
-                    off[o][j] = (unsigned)(depth + (j & 1) * 32) * ld + (f < end ? f : 0) * 2;
-                } else {
-                    int r = (j * kWaves + wave) * 8 + (lane >> 3);
-                    if (!o && GATED) r &= HALF - 1;
-                    off[o][j] = r < end ? (unsigned)r * ld + chunk * 16 : o ? kNowhere : (unsigned)chunk * 16;
-                }
-            }
-            steps_here[o] = trans ? (k - depth + 63) / 64 : (k * size - chunk * 16 + kStep - 1) / kStep;
-        }
-        const char *a0, *a1, *b0;                                      // a1: ups of a gated tile
-        if (FORM == kWeightGradient) a0 = P.a + (size_t)rows.first * P.a_ld + f0 * 2;
-        else a0 = P.a + (size_t)e * P.a_expert + (kTransA ? (size_t)f0 * 2 : (size_t)f0 * P.a_ld);
-        a1 = GATED ? a0 + (size_t)P.features * P.a_ld : a0;
-        b0 = kTransB ? P.b + (size_t)rows.first * P.b_ld + r0 * 2 : P.b + (size_t)(rows.first + r0) * P.b_ld;
-        // (weights never change while a kernel runs: scalar loads)
+        int depth;                                 // transposed: row of this lane's chunk of a unit's first load
+        const char *a0, *a1, *b0;                  // a1: ups of a gated tile
+        // e4m3: scales of 128 features (weights never change while a kernel runs: scalar loads) and of the rows, one a step
         typedef const __attribute__((address_space(4))) float *Constant;
         Constant sa[2] = {nullptr, nullptr};
         const char *sb = nullptr;
         unsigned off_s = 0;
         const int per_row = P.k / 128;
-        if (E4M3) {                                                    // scales: of a row and of 128 features, one a step
-            const int blocks = (P.features + 127) / 128;
-            const Constant first = (Constant)(uintptr_t)P.a_scales + (size_t)e * blocks * (GATED ? 2 : 1) * per_row;
-            const int block = f0 / 128, second = (f0 + HALF) / 128;
-            sa[0] = first + (size_t)block * per_row;
-            sa[1] = first + (size_t)(GATED ? blocks + block : second < blocks ? second : block) * per_row;
-            sb = (const char *)(P.b_scales + (size_t)(rows.first + r0) * per_row);
-            // this wave's in B0, then in B1; of 64 rows each wave a share
-            int r = ROWS == 256 ? (lane >> 5) * kUnitRows + wr * 32 + (lane & 31) : wave * kLoadsB * 8 + (lane & (kLoadsB * 8 - 1));
-            if (r >= n_b - r0) r = 0;
-            off_s = (unsigned)r * per_row * 4;
-        }
+        auto set_out = [&]() FLMOE_INLINE {
+            // (opaque, so that what follows from it is worked out here and not kept in registers from tile to tile)
+            int l = lane;
+            asm volatile("" : "+v"(l));
+            const int e = tile.e, f0 = tile.f0, r0 = tile.r0;
+            const Rows rows = tile.rows;
+            k = FORM == kWeightGradient ? rows.n : P.k;
+            n_b = FORM == kWeightGradient ? P.other : rows.n;
+            steps = (int)(((long long)k * size + kStep - 1) / kStep);
+            few = kHalves == 1 || n_b - r0 <= kUnitRows;
+            shift = (int)((long long)blockIdx.x * steps / gridDim.x);
+            depth = wave * 4 + (l >> 4);
+            const int column = ((l & 15) ^ spread(depth)) * 8;
+#pragma unroll
+            for (int o = 0; o < 2; ++o) {
+                const bool trans = o ? kTransB : kTransA;
+                const int ld = o ? P.b_ld : P.a_ld, end = o ? n_b - r0 : P.features - f0;
+                const int chunk = (l & 7) ^ swizzle(wave * 8 + (l >> 3));               // contiguous along the contraction
+#pragma unroll
+                for (int j = 0; j < (o ? kHalves * kLoadsB : 4); ++j) {
+                    if (trans) {
+                        const int f = (j >> 1) * HALF + column;
+                        off[o][j] = (unsigned)(depth + (j & 1) * 32) * ld + (f < end ? f : 0) * 2;
+                    } else {
+                        int r = (j * kWaves + wave) * 8 + (l >> 3);
+                        if (!o && GATED) r &= HALF - 1;
+                        off[o][j] = r < end ? (unsigned)r * ld + chunk * 16 : o ? kNowhere : (unsigned)chunk * 16;
+                    }
+                }
+                steps_here[o] = trans ? (k - depth + 63) / 64 : (k * size - chunk * 16 + kStep - 1) / kStep;
+            }
+            if (FORM == kWeightGradient) a0 = P.a + (size_t)rows.first * P.a_ld + f0 * 2;
+            else a0 = P.a + (size_t)e * P.a_expert + (kTransA ? (size_t)f0 * 2 : (size_t)f0 * P.a_ld);
+            a1 = GATED ? a0 + (size_t)P.features * P.a_ld : a0;
+            b0 = kTransB ? P.b + (size_t)rows.first * P.b_ld + r0 * 2 : P.b + (size_t)(rows.first + r0) * P.b_ld;
+            if (E4M3) {
+                const int blocks = (P.features + 127) / 128;
+                const Constant first = (Constant)(uintptr_t)P.a_scales + (size_t)e * blocks * (GATED ? 2 : 1) * per_row;
+                const int block = f0 / 128, second = (f0 + HALF) / 128;
+                sa[0] = first + (size_t)block * per_row;
+                sa[1] = first + (size_t)(GATED ? blocks + block : second < blocks ? second : block) * per_row;
+                sb = (const char *)(P.b_scales + (size_t)(rows.first + r0) * per_row);
+                // this wave's in B0, then in B1; of 64 rows each wave a share
+                int r = ROWS == 256 ? (l >> 5) * kUnitRows + wr * 32 + (l & 31) : wave * kLoadsB * 8 + (l & (kLoadsB * 8 - 1));
+                if (r >= n_b - r0) r = 0;
+                off_s = (unsigned)r * per_row * 4;
+            }
+        };
 
         const unsigned lds0 = lds_address(lds);
         // [slot][A0, A1], then [slot][B0, B1]: what one operand's reads span fits their instructions' offset
@@ -347,17 +367,6 @@ struct Tile {
             }
         };
         Acc acc[2][kHalves][kFragsF][kFragsR];
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int g = 0; g < kHalves; ++g)
-#pragma unroll
-                for (int i = 0; i < kFragsF; ++i)
-#pragma unroll
-                    for (int j = 0; j < kFragsR; ++j)
-#pragma unroll
-                        for (int t = 0; t < 4; ++t) acc[h][g][i][j][t] = 0.0f;
-
         Frag fa[kFragsF][kParts], fb0[2][kFragsR][kParts], fb1[kFragsR][kParts];
         float row_scale[kFragsR];
         // multiplies the fragments at hand into quadrant (h, g); next(i, part) follows a fragment's last use
@@ -432,18 +441,12 @@ struct Tile {
             multiply(half_a, half_b, b, w, [&](int i, int part) FLMOE_INLINE { fa[i][part] = frag(Zero(), base, i, part); });
         };
 
-        __syncthreads();                           // the tile before is done with its LDS
         auto two_units = [&](auto one) FLMOE_INLINE {                  // (a template, so that it is made where it is called only)
             using One = decltype(one);
             // Loads of this wave that may still be on their way between phases: all but the units that the next phase reads
             // and those before them, four units of two loads, and in e4m3 a load of scales among them.
             constexpr int kAhead = E4M3 ? 9 : 8;
             Straight t;
-#pragma unroll
-            for (int step = 0; step < 2; ++step) {
-                load_scales(step, t);
-                load(B0, step, t); load(A0, step, t); load(B1, step, t); load(A1, step, t);
-            }
             loads_done_and_barrier<kAhead + 4>();
             read_a(0);
             read_b(fb0[0], 0);
@@ -479,10 +482,6 @@ struct Tile {
             // whose rows there are none of only load.
             constexpr int kAhead = 4 + kLoadsB + (E4M3 ? 1 : 0);
             Turned t;
-#pragma unroll
-            for (int step = 0; step < 2; ++step) {
-                load(B0, step, t); load_scales(step, t); load(A0, step, t); load(A1, step, t);
-            }
             loads_done_and_barrier<kAhead + 2>();
             auto start = [&]() FLMOE_INLINE {
                 loads_done_and_barrier<kAhead>();
@@ -513,7 +512,7 @@ struct Tile {
                     body(step + 1, One(), present);
                 }
             };
-            if (kWavesR == 1 || wr * kOwnR < n_b - r0) {
+            if (kWavesR == 1 || wr * kOwnR < n_b - tile.r0) {
                 read_a(0);
                 read_b(fb0[0], 0);
                 start();
@@ -523,81 +522,163 @@ struct Tile {
                 all(Zero());
             }
         };
-        if constexpr (kHalves == 1) one_unit();
-        else if (few) one_unit();
-        else two_units(One());
-        loads_done_and_barrier<0>();               // also those of steps that are none
+        // the tile's first loads: what the loops above begin with
+        auto begin = [&]() FLMOE_INLINE {
+#pragma unroll
+            for (int step = 0; step < 2; ++step) {
+                if (few) {
+                    Turned t;
+                    load(B0, step, t); load_scales(step, t); load(A0, step, t); load(A1, step, t);
+                } else if constexpr (kHalves == 2) {
+                    Straight t;
+                    load_scales(step, t); load(B0, step, t); load(A0, step, t); load(B1, step, t); load(A1, step, t);
+                }
+            }
+        };
 
-        // ---- the tile's output, HALF features at a time through LDS, so that rows are written in whole lines
-        float *out = (float *)lds;
-        tid = threadIdx.x;
-        asm volatile("" : "+v"(tid));
-        lane = tid & (kWave - 1);
-        constexpr int kPieces = HALF / 8;                              // of eight features, a lane each
-        const int piece = tid & (kPieces - 1), n_rows = n_b - r0 < ROWS ? n_b - r0 : ROWS;
-        // Moves value(g, i, j, t) of a half of the features to LDS and from there, eight features a lane, to put(row, values).
-        auto emit = [&](auto value, auto put) FLMOE_INLINE {
-            __syncthreads();
+        // ---- the tile's output: accumulators hold four features of a row a lane, memory wants whole lines
+        float *largest = (float *)(lds + kLargestAt);                  // [kWavesF][ROWS]
+        int el;                                                        // lane
+        // Moves value(g, i, j, t) of a half of the features to put(row, values), eight features a lane.
+        auto emit = [&](int n_rows, auto value, auto put) FLMOE_INLINE {
+            float *mine = (float *)(lds + kEmitAt) + wave * kEmitRows * kEmitPitch;
+            const int piece = el & (kPieces - 1);
 #pragma unroll
             for (int g = 0; g < kHalves; ++g)
 #pragma unroll
-                for (int i = 0; i < kFragsF; ++i)
+                for (int first = 0; first < kOwnR; first += kEmitRows) {
 #pragma unroll
                     for (int j = 0; j < kFragsR; ++j) {
-                        const int row = g * kUnitRows + wr * kOwnR + j * kSide + (lane & 15), f = wf * kOwnF + i * kSide + (lane >> 4) * 4;
-                        const v4f v = {value(g, i, j, 0), value(g, i, j, 1), value(g, i, j, 2), value(g, i, j, 3)};
-                        *(v4f *)(out + row * kEmitPitch + f) = v;
+                        const int row = j * kSide + (el & 15) - first;
+                        if (j * kSide + kSide <= first || j * kSide >= first + kEmitRows) continue;
+                        if (row >= 0 && row < kEmitRows) {
+#pragma unroll
+                            for (int i = 0; i < kFragsF; ++i)
+                                *(v4f *)(mine + row * kEmitPitch + i * kSide + (el >> 4) * 4) =
+                                    v4f{value(g, i, j, 0), value(g, i, j, 1), value(g, i, j, 2), value(g, i, j, 3)};
+                        }
                     }
-            __syncthreads();
-            for (int row = tid / kPieces; row < n_rows; row += kThreads / kPieces) {
-                const v4f x = *(const v4f *)(out + row * kEmitPitch + piece * 8), y = *(const v4f *)(out + row * kEmitPitch + piece * 8 + 4);
-                const float v[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
-                put(row, v);
-            }
+                    asm volatile("" ::: "memory");         // (a wave's reads of LDS follow its writes)
+                    const float *from = mine + (el / kPieces) * kEmitPitch + piece * 8;
+                    const v4f x = *(const v4f *)from, y = *(const v4f *)(from + 4);
+                    const float v[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+                    const int row = g * kUnitRows + wr * kOwnR + first + el / kPieces;
+                    if (row < n_rows) put(row, v);
+                    asm volatile("" ::: "memory");
+                }
         };
         // the eight features from f on of row `row` of a tensor `width` features wide
         auto put_bf16 = [&](void *to, size_t row, int f, int width, const float *v) {
             const v4u w = {to_bf16x2(v[0], v[1]), to_bf16x2(v[2], v[3]), to_bf16x2(v[4], v[5]), to_bf16x2(v[6], v[7])};
             *(v4u *)((char *)to + (row * width + f) * 2) = w;
         };
-        auto put_e4m3 = [&](void *to, float *scales, size_t row, int f, int width, const float *v) {
-            float amax = 0.0f;                                         // NaN fails the comparison and is skipped
+        // in blocks of e4m3; the tile's 128 features are one block
+        auto find_largest = [&](auto value) FLMOE_INLINE {
+            __syncthreads();                                           // those found before have been read
 #pragma unroll
-            for (int i = 0; i < 8; ++i) amax = fabsf(v[i]) > amax ? fabsf(v[i]) : amax;
+            for (int g = 0; g < kHalves; ++g)
 #pragma unroll
-            for (int o = 1; o < kPieces; o <<= 1) amax = fmaxf(amax, __shfl_xor(amax, o));
-            const float scale = block_scale(amax);
-            const v2u w = {e4m3_codes(v, scale), e4m3_codes(v + 4, scale)};
-            *(v2u *)((char *)to + row * width + f) = w;
-            if (piece == 0) scales[row * (width / 128) + f / 128] = scale;
+                for (int j = 0; j < kFragsR; ++j) {
+                    float m = 0.0f;                                    // NaN fails the comparison and is skipped
+#pragma unroll
+                    for (int i = 0; i < kFragsF; ++i)
+#pragma unroll
+                        for (int t = 0; t < 4; ++t) { const float v = fabsf(value(g, i, j, t)); m = v > m ? v : m; }
+                    m = fmaxf(m, __shfl_xor(m, 16));
+                    m = fmaxf(m, __shfl_xor(m, 32));
+                    if (el < kSide) largest[wf * ROWS + g * kUnitRows + wr * kOwnR + j * kSide + el] = m;
+                }
+            __syncthreads();
         };
-        // output row of the tile's first row
-        const size_t row0 = FORM == kWeightGradient ? (size_t)e * P.other + r0 : (size_t)(rows.first + r0);
-        const int f = f0 + piece * 8;
-        if constexpr (GATED) {
-            if (P.pre) {
+        auto put_e4m3 = [&](void *to, float *scales, size_t row0, int row, int f, int width, const float *v) {
+            float m = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kWavesF; ++i) m = fmaxf(m, largest[i * ROWS + row]);
+            const float scale = block_scale(m);
+            const v2u w = {e4m3_codes(v, scale), e4m3_codes(v + 4, scale)};
+            *(v2u *)((char *)to + (row0 + row) * width + f) = w;
+            if (wf == 0 && (el & (kPieces - 1)) == 0) scales[(row0 + row) * (width / 128) + f / 128] = scale;
+        };
+        auto write = [&](const Place &done) FLMOE_INLINE {
+            el = lane;
+            asm volatile("" : "+v"(el));                               // as in set_out
+            const int end = FORM == kWeightGradient ? P.other : done.rows.n, n_rows = end - done.r0 < ROWS ? end - done.r0 : ROWS;
+            // output row of the tile's first row
+            const size_t row0 = FORM == kWeightGradient ? (size_t)done.e * P.other + done.r0 : (size_t)(done.rows.first + done.r0);
+            const int f = done.f0 + wf * kOwnF + (el & (kPieces - 1)) * 8;
+            if constexpr (GATED) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    if (!P.pre) break;
+                    auto value = [&](int g, int i, int j, int t) { return acc[h][g][i][j][t]; };
+                    if (P.pre_scales) {
+                        find_largest(value);
+                        emit(n_rows, value, [&](int row, const float *v) {
+                            put_e4m3(P.pre, P.pre_scales, row0, row, h * P.features + f, 2 * P.features, v);
+                        });
+                    } else {
+                        emit(n_rows, value, [&](int row, const float *v) {
+                            if (f < P.features) put_bf16(P.pre, row0 + row, h * P.features + f, 2 * P.features, v);
+                        });
+                    }
+                }
+#pragma unroll
+                for (int g = 0; g < kHalves; ++g)
+#pragma unroll
+                    for (int i = 0; i < kFragsF; ++i)
+#pragma unroll
+                        for (int j = 0; j < kFragsR; ++j)
+#pragma unroll
+                            for (int t = 0; t < 4; ++t)
+                                acc[0][g][i][j][t] = activate<false>(P.act, acc[0][g][i][j][t], nullptr) * acc[1][g][i][j][t];
+                auto value = [&](int g, int i, int j, int t) { return acc[0][g][i][j][t]; };
+                if constexpr (E4M3) {
+                    find_largest(value);
+                    emit(n_rows, value, [&](int row, const float *v) { put_e4m3(P.out, P.out_scales, row0, row, f, P.features, v); });
+                } else {
+                    emit(n_rows, value, [&](int row, const float *v) {
+                        if (f < P.features) put_bf16(P.out, row0 + row, f, P.features, v);
+                    });
+                }
+            } else {
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
-                    emit([&](int g, int i, int j, int t) { return acc[h][g][i][j][t]; },
+                    emit(n_rows, [&](int g, int i, int j, int t) { return acc[h][g][i][j][t]; },
                          [&](int row, const float *v) {
-                             if (f >= P.features) return;
-                             if (P.pre_scales) put_e4m3(P.pre, P.pre_scales, row0 + row, h * P.features + f, 2 * P.features, v);
-                             else put_bf16(P.pre, row0 + row, h * P.features + f, 2 * P.features, v);
+                             if (f + h * HALF < P.features) put_bf16(P.out, row0 + row, f + h * HALF, P.features, v);
                          });
             }
-            emit([&](int g, int i, int j, int t) { return activate<false>(P.act, acc[0][g][i][j][t], nullptr) * acc[1][g][i][j][t]; },
-                 [&](int row, const float *v) {
-                     if (f >= P.features) return;
-                     if (E4M3) put_e4m3(P.out, P.out_scales, row0 + row, f, P.features, v);
-                     else put_bf16(P.out, row0 + row, f, P.features, v);
-                 });
-        } else {
+        };
+
+        if (!next_place(&tile)) return;
+        set_out();
+        begin();
+        for (;;) {
 #pragma unroll
             for (int h = 0; h < 2; ++h)
-                emit([&](int g, int i, int j, int t) { return acc[h][g][i][j][t]; },
-                     [&](int row, const float *v) {
-                         if (f + h * HALF < P.features) put_bf16(P.out, row0 + row, f + h * HALF, P.features, v);
-                     });
+#pragma unroll
+                for (int g = 0; g < kHalves; ++g)
+#pragma unroll
+                    for (int i = 0; i < kFragsF; ++i)
+#pragma unroll
+                        for (int j = 0; j < kFragsR; ++j) acc[h][g][i][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+            if constexpr (kHalves == 1) one_unit();
+            else if (few) one_unit();
+            else two_units(One());
+            loads_done_and_barrier<0>();           // also those of steps that are none; and the ring is free
+            const Place done = tile;
+            const bool more = next_place(&tile);
+            if (kEarly && more) {
+                set_out();
+                begin();
+            }
+            write(done);
+            if (!more) break;
+            if (!kEarly) {
+                __syncthreads();                   // the output is out of the ring
+                set_out();
+                begin();
+            }
         }
     }
 };
@@ -644,30 +725,36 @@ __global__ __launch_bounds__((Tile<FORM, E4M3, GATED, ROWS, HALF>::kThreads), 2)
     // Workgroups go to the XCDs in turn.  Each XCD has an eighth of the tiles, neighbours, whose operands its L2 then holds.
     const int xcd = blockIdx.x % kXcds;
     const long long end = tiles * (xcd + 1) / kXcds;
-    for (long long t = tiles * xcd / kXcds + blockIdx.x / kXcds; t < end; t += gridDim.x / kXcds) {
-        const int row_tile = (int)(t / columns);                       // counted over the experts
-        int lo = 0, hi = G.n, n_tiles, index;
-        if constexpr (FORM == kWeightGradient) {
-            lo = row_tile / fixed;
-            n_tiles = fixed;
-            index = (int)(t - (long long)lo * fixed * columns);
-        } else {
-            while (hi - lo > 1) {
-                const int mid = (lo + hi) >> 1;
-                if (before[mid] <= row_tile) lo = mid; else hi = mid;
+    long long t = tiles * xcd / kXcds + blockIdx.x / kXcds;
+    T::run(P, lds, [&](typename T::Place *to) {
+        for (; t < end; t += gridDim.x / kXcds) {
+            const int row_tile = (int)(t / columns);                   // counted over the experts
+            int lo = 0, hi = G.n, n_tiles, index;
+            if constexpr (FORM == kWeightGradient) {
+                lo = row_tile / fixed;
+                n_tiles = fixed;
+                index = (int)(t - (long long)lo * fixed * columns);
+            } else {
+                while (hi - lo > 1) {
+                    const int mid = (lo + hi) >> 1;
+                    if (before[mid] <= row_tile) lo = mid; else hi = mid;
+                }
+                n_tiles = before[lo + 1] - before[lo];
+                index = (int)(t - (long long)before[lo] * columns);
             }
-            n_tiles = before[lo + 1] - before[lo];
-            index = (int)(t - (long long)before[lo] * columns);
+            const int group = index / (kRowGroup * columns), left = n_tiles - group * kRowGroup;
+            const int in_group = left < kRowGroup ? left : kRowGroup, within = index - group * kRowGroup * columns;
+            const int column = within / in_group, row = group * kRowGroup + within - column * in_group;
+            const int e = G.first + __builtin_amdgcn_readfirstlane(lo);
+            const Rows found = rows_of(G, e), rows = {same_in_wave(found.first), __builtin_amdgcn_readfirstlane(found.n)};
+            // (tables that claim more rows than there can be may have wrapped the sums)
+            if ((unsigned)column >= (unsigned)columns || row < 0 || (long long)row * ROWS >= (FORM == kWeightGradient ? P.other : rows.n)) continue;
+            *to = {e, rows, __builtin_amdgcn_readfirstlane(column) * T::kOutput, __builtin_amdgcn_readfirstlane(row) * ROWS};
+            t += gridDim.x / kXcds;
+            return true;
         }
-        const int group = index / (kRowGroup * columns), left = n_tiles - group * kRowGroup;
-        const int in_group = left < kRowGroup ? left : kRowGroup, within = index - group * kRowGroup * columns;
-        const int column = within / in_group, row = group * kRowGroup + within - column * in_group;
-        const int e = G.first + __builtin_amdgcn_readfirstlane(lo);
-        const Rows found = rows_of(G, e), rows = {same_in_wave(found.first), __builtin_amdgcn_readfirstlane(found.n)};
-        // (tables that claim more rows than there can be may have wrapped the sums)
-        if ((unsigned)column >= (unsigned)columns || row < 0 || (long long)row * ROWS >= (FORM == kWeightGradient ? P.other : rows.n)) continue;
-        T::run(P, lds, e, rows, __builtin_amdgcn_readfirstlane(column) * T::kOutput, __builtin_amdgcn_readfirstlane(row) * ROWS);
-    }
+        return false;
+    });
 }
 
 // ---------------------------------------------------------------- the gated block's own gradient
