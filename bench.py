@@ -203,6 +203,36 @@ def interleaved_caller_work(workloads, harness, torch, steps=100, rounds=3):
     return out
 
 
+def layer_with_experts(workloads, harness, torch, name, inter, steps, warmup):
+    """A whole mixture-of-experts layer of one workload: the five calls with the experts' products (gated block of width
+    `inter`, projection back; e4m3 on a workload that dispatches e4m3) between dispatch and combine, on one stream; and the
+    products alone.  Random weights."""
+    wl = workloads.WORKLOADS[name]
+    inp = workloads.make_inputs(wl)
+    dev = harness.to_device(inp, "cuda:0")
+    sh = harness.make_shuffle(inp, capacity_factor=None if wl.zipf_alpha > 0 else 1.1 if wl.tokens >= 2048 else 1.5)
+    ex, weights = harness.make_experts(sh, inter)
+    pairs = workloads.describe(inp)["pairs"]
+
+    def timed(step):
+        for _ in range(warmup):
+            step()
+        torch.cuda.synchronize()
+        t0 = time.perf_counter()
+        for _ in range(steps):
+            step()
+        torch.cuda.synchronize()
+        return (time.perf_counter() - t0) * 1e3 / steps
+    layer_ms = timed(lambda: harness.run_layer(sh, ex, weights, dev))
+    assert sh.status() == 0
+    experts_ms = timed(lambda: ex.forward(*weights))
+    flops = 6 * pairs * inter * wl.hidden
+    moved = sum(t.numel() * t.element_size() for t in weights) + pairs * (sh.sizes.expert_x_row_bytes + 2 * wl.hidden)
+    sh.close()
+    return {"ms_per_step": round(layer_ms, 4), "experts_ms": round(experts_ms, 4), "inter": inter, "pairs": pairs,
+            "experts_tflops": round(flops / experts_ms / 1e9, 1), "experts_gbps": round(moved / experts_ms / 1e6, 1)}
+
+
 def ordering_name(args):
     if args.stream_ordered:
         return "stream order supplied by the caller (no announce, no gate kernels)"
@@ -253,6 +283,9 @@ def main():
     ap.add_argument("--interleaved", action="store_true",
                     help="only the decode step with a caller's matrix products on a second stream between "
                          "the send and receive halves (the side measurement interleaved_caller_work)")
+    ap.add_argument("--experts", type=int, default=0, metavar="INTER",
+                    help="only a whole layer of the workload: the step with the experts' products (gated block of this "
+                         "width) between dispatch and combine")
     args = ap.parse_args()
     if args.gpus != 1:
         print("bench.py: this build runs the whole simulated expert-parallel group on ONE GPU; "
@@ -268,6 +301,14 @@ def main():
         print(json.dumps({"metric": "interleaved_caller_work", "ms_per_step": round(res["together_us"] / 1e3, 4),
                           "config": {"workload": "dsv3_decode"}, "library_build_id": flmoe.fl_moe_build_id(),
                           "interleaved_caller_work": res}))
+        return
+
+    if args.experts:
+        res = layer_with_experts(workloads, harness, torch, args.workload, args.experts, args.steps or 50,
+                                 args.warmup if args.warmup >= 0 else 10)
+        print(json.dumps({"metric": "layer_with_experts", "ms_per_step": res["ms_per_step"],
+                          "config": {"workload": args.workload}, "library_build_id": flmoe.fl_moe_build_id(),
+                          "layer_with_experts": res}))
         return
 
     wl = workloads.WORKLOADS[args.workload]

@@ -574,3 +574,76 @@ class MoEShuffle:
             "buf_a": self.table(dv.buf_a, (N, dv.buf_a_rank_bytes), torch.uint8),
             "buf_b": self.table(dv.buf_b, (N, dv.buf_b_rank_bytes), torch.uint8),
         }
+
+
+class MoEExperts:
+    """The experts of one layer between dispatch_recv and combine_send of a MoEShuffle: owns their rows' buffers and
+    forwards to the C calls.  No arithmetic happens here.
+
+    inter: width of the gated block; w_in [E][2 * inter][hidden] (gates, then ups), w_out [E][hidden][inter]; bf16, or for
+    a shuffle with e4m3 dispatch e4m3 codes with the scales of their 128 x 128 blocks (inference only).
+    training: keeps what the backward pass needs: the pre-activations in bf16 or, keep="e4m3", in 8-bit blocks (then the
+    block's output is not kept either, but worked out again), and copies of the step's tables, so that other layers'
+    steps may run in between.  The rows themselves (expert_x) are the caller's to keep."""
+
+    def __init__(self, shuffle, inter, activation="silu", training=False, keep="bf16"):
+        self.shuffle, self.inter, self.training, self.keep = shuffle, inter, training, keep
+        self.activation = {"silu": FL_ACT_SILU, "gelu": FL_ACT_GELU}[activation]
+        self.e4m3 = shuffle.expert_scales is not None
+        if keep not in ("bf16", "e4m3") or (training and self.e4m3):
+            raise FlMoeError(FL_ERR_INVALID_ARG, "MoEExperts: rows of e4m3 have no backward pass; keep is bf16 or e4m3")
+
+        def rows(width, dtype=torch.bfloat16):
+            return torch.empty((shuffle.N, shuffle.expert_capacity_rows, width), dtype=dtype, device=shuffle.device)
+        self.h = rows(inter, torch.uint8 if self.e4m3 else torch.bfloat16)
+        self.h_scales = rows(inter // 128, torch.float32) if self.e4m3 else None
+        self.y = rows(shuffle.H)
+        self.pre = self.pre_scales = self.tables = None
+        if training:
+            eights = keep == "e4m3"
+            self.pre = rows(2 * inter, torch.uint8 if eights else torch.bfloat16)
+            self.pre_scales = rows(2 * inter // 128, torch.float32) if eights else None
+            # the pre-activations' gradients take the place of what was kept where they fit
+            self.dpre = rows(2 * inter) if eights else self.pre
+            self.dh, self.dx = rows(inter), rows(shuffle.H)
+
+    def _at(self, ranks):
+        rb, rc = self.shuffle._ranks(ranks)
+        return (self.shuffle.cfg, rb, rc, *self.tables)
+
+    def forward(self, w_in, w_out, in_scales=None, out_scales=None, x=None, ranks=None, stream=None):
+        """y of the rows that dispatch_recv left (x: of other rows in that layout)."""
+        sh = self.shuffle
+        if self.training:
+            on = torch.cuda.current_stream(sh.device) if stream is None else stream
+            with torch.cuda.stream(on):
+                tabs = sh.layout_tables()
+                if self.tables is None:
+                    self.tables = [torch.empty_like(tabs["expert_off"]), torch.empty_like(tabs["G"])]
+                self.tables[0].copy_(tabs["expert_off"])
+                self.tables[1].copy_(tabs["G"])
+        else:
+            self.tables = (sh.view.expert_off, sh.view.tokens_per_expert)
+        at, x = self._at(ranks), sh.expert_x if x is None else x
+        if self.e4m3:
+            fl_moe_expert_gated_e4m3(*at, self.inter, self.activation, x, sh.expert_scales, w_in, in_scales, self.h,
+                                     self.h_scales, stream)
+            fl_moe_expert_product_e4m3(*at, self.inter, sh.H, self.h, self.h_scales, w_out, out_scales, self.y, stream)
+        else:
+            fl_moe_expert_gated(*at, self.inter, self.activation, x, w_in, self.h, self.pre, self.pre_scales, stream)
+            fl_moe_expert_product(*at, self.inter, sh.H, self.h, w_out, self.y, stream)
+        return self.y
+
+    def backward(self, dy, w_in, w_out, dw_in, dw_out, x=None, ranks=None, stream=None):
+        """The rows' gradient; the weights' go to dw_in and dw_out.  Once per forward: with bf16 the kept pre-activations are
+        gone then.  x: the rows that forward had."""
+        sh, at = self.shuffle, self._at(ranks)
+        x = sh.expert_x if x is None else x
+        again = self.h if self.keep == "e4m3" else None
+        fl_moe_expert_product_backward(*at, self.inter, sh.H, self.h, w_out, dy, self.dh, None if again is not None else dw_out,
+                                       stream)
+        fl_moe_expert_gated_backward(*at, self.inter, self.activation, x, w_in, self.pre, self.pre_scales, self.dh, self.dpre,
+                                     self.dx, dw_in, again, stream)
+        if again is not None:
+            fl_moe_expert_product_backward(*at, self.inter, sh.H, again, None, dy, None, dw_out, stream)
+        return self.dx

@@ -161,3 +161,37 @@ def run_chunked(sh: flmoe.MoEShuffle, chunks, out_full: torch.Tensor, identity=F
         out = sh.combine_reduce(dev["weights"])
         out_full[:, t0:t0 + n].copy_(out[:, :n])
     return out_full
+
+
+def make_experts(sh: flmoe.MoEShuffle, inter, seed=0, **kw):
+    """(MoEExperts, its weights as forward takes them): random weights of the scale that keeps rows at theirs."""
+    ex = flmoe.MoEExperts(sh, inter, **kw)
+    g = torch.Generator(device=sh.device).manual_seed(seed)
+    shapes = ((sh.E, 2 * inter, sh.H), (sh.E, sh.H, inter))
+    if not ex.e4m3:
+        return ex, tuple(torch.randn(s, generator=g, device=sh.device, dtype=torch.bfloat16) / s[2] ** 0.5 for s in shapes)
+    codes = tuple((torch.randn(s, generator=g, device=sh.device, dtype=torch.bfloat16) * 100).clamp_(-448, 448)
+                  .to(torch.float8_e4m3fn) for s in shapes)
+    scales = tuple(torch.full((s[0], -(-s[1] // 128), s[2] // 128), 0.01 / s[2] ** 0.5, device=sh.device) for s in shapes)
+    return ex, codes + scales
+
+
+def run_layer(sh: flmoe.MoEShuffle, ex: flmoe.MoEExperts, weights, dev):
+    """One step of a mixture-of-experts layer: the five calls with the experts' products in the place of the stand-in."""
+    sh.layout(dev["indices"], dev["num_tokens"])
+    sh.dispatch_send(dev["x"], weights=send_weights(sh, dev))
+    sh.dispatch_recv()
+    sh.combine_send(ex.forward(*weights))
+    return sh.combine_reduce(dev["weights"])
+
+
+def run_layer_backward(sh: flmoe.MoEShuffle, ex: flmoe.MoEExperts, weights, grads, dev, x, dout, row_weights, ones):
+    """The layer's backward pass, a step of its own: the gradient of `out` goes the way the tokens went (dispatch), each
+    row of it times the row's routing weight is the gradient of y, and the rows' gradients come back the way the replies
+    came (combine with weights of one).  x: a copy of the rows that the forward pass had in expert_x, which the gradient's
+    rows overwrite; row_weights [N][capacity] fp32: the routing weight of each expert row; ones: dev["weights"]' shape."""
+    sh.layout(dev["indices"], dev["num_tokens"])
+    sh.dispatch_send(dout)
+    dy = (sh.dispatch_recv().float() * row_weights[..., None]).to(torch.bfloat16)
+    sh.combine_send(ex.backward(dy, *weights, *grads, x=x))
+    return sh.combine_reduce(ones, out=torch.empty_like(sh.out))

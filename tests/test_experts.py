@@ -3,7 +3,13 @@
 Tolerances are bounds, derived here once.  A sum of k products in fp32, in any order, each step off by at most one unit
 in the last place (2^-23) of what has been summed: off by at most k 2^-23 sum |a b|.  A result rounded to bf16: half a
 step, 2^-8 of the value; to an e4m3 block: 2^-4 of the value or half the smallest step, 2^-10 of the scale.
-Inputs of bf16 or e4m3 are exact in 64 bits."""
+Inputs of bf16 or e4m3 are exact in 64 bits.
+
+The matrix instruction for e4m3 adds the products of eight neighbours of the contraction after it has cut each of them,
+towards zero, 13 binary places below the first place of the largest of the eight (measured: beside a product of 2^16 one
+of 2^3 is kept whole, one of 1.875 * 2^3 becomes 2^3, one of 2^2 is lost; beside one of 1.875^2 * 2^14 one of 2^1 is kept;
+in another group of eight any is).  The largest itself, of 8 significant places, is not cut.  So a group is off by less
+than 7 * 2^-13 of its largest product, which is at most the product of the largest values of both sides there (`cut`)."""
 import ctypes as C
 import math
 
@@ -199,11 +205,11 @@ def act_off(v, act, dv):
     return SLOPE * dv + (a.abs() + dv) * U * (16 + 8 * arg.abs())
 
 
-def gated64(x, w, act, steps=None):
-    """g, u, h and how far fp32 sums of `steps` additions leave g, u, h off, before rounding."""
+def gated64(x, w, act, steps=None, off=0.0):
+    """g, u, h and how far fp32 sums of `steps` additions (and `off` besides) leave g, u, h off, before rounding."""
     i = w.shape[0] // 2
     p, size = x @ w.T, x.abs() @ w.abs().T
-    dp = (steps or x.shape[1]) * U * size
+    dp = (steps or x.shape[1]) * U * size + off
     g, u, dg, du = p[:, :i], p[:, i:], dp[:, :i], dp[:, i:]
     a = act64(g, act)[0]
     da = act_off(g, act, dg)
@@ -361,6 +367,12 @@ E4M3_SHAPES = [([[1]], 128, 128), ([[3, 0]], 256, 384), ([[16, 17, 0, 1], [0, 0,
                ([[127, 128, 129]], 512, 256), ([[255, 0, 257], [256, 2, 511]], 256, 640), ([[9, 700]], 2048, 128)]
 
 
+def cut(x, w):
+    """What the matrix instruction may cut off the products' sums (see above)."""
+    largest = lambda v: v.abs().unflatten(1, (-1, 8)).amax(-1)
+    return 7 * 2.0 ** -13 * (largest(x) @ largest(w).T)
+
+
 def sums(k):
     """Steps of a sum over e4m3 blocks: 128 products in a block, a multiplication of the scales, one addition a block."""
     return 128 + 3 + k // 128
@@ -377,7 +389,8 @@ def test_gated_e4m3(counts, hidden, inter, act):
     want, off = {}, {}
     for d, j in L.experts():
         rows = L.span(d, j)
-        _, _, want[d, j], off[d, j] = gated64(dequantised(x[d, rows], xs[d, rows]), w64[d * L.el + j], act, sums(hidden))
+        x64, we = dequantised(x[d, rows], xs[d, rows]), w64[d * L.el + j]
+        _, _, want[d, j], off[d, j] = gated64(x64, we, act, sums(hidden), cut(x64, we))
     check_blocks(L, h, hs, want, off, "h")
 
 
@@ -393,7 +406,7 @@ def test_product_e4m3(counts, in_, out):
         rows = L.span(d, j)
         x64, we = dequantised(x[d, rows], xs[d, rows]), w64[d * L.el + j]
         want[d, j] = x64 @ we.T
-        tol[d, j] = want[d, j].abs() * BF16 + (1 + BF16) * sums(in_) * U * (x64.abs() @ we.abs().T) + TINY
+        tol[d, j] = want[d, j].abs() * BF16 + (1 + BF16) * (sums(in_) * U * (x64.abs() @ we.abs().T) + cut(x64, we)) + TINY
     L.check_rows(y, want, tol, "y")
 
 
@@ -599,3 +612,197 @@ def test_the_binding_refuses_wrong_tensors():
         with pytest.raises(flmoe.FlMoeError) as e:
             flmoe.fl_moe_expert_gated(*args)
         assert e.value.code == INVALID, place
+
+
+# ------------------------------------------------------------------ together with the shuffle
+def layer_inputs(**kw):
+    from paper_2510_27656_amd import harness, workloads
+    wl = workloads.custom("layer", 4, 16, 37, 256, 4, seed=5, ragged=True, **kw)
+    inp = workloads.make_inputs(wl)
+    return wl, inp, harness.to_device(inp), harness
+
+
+def tokens_by_expert(wl, inp):
+    """(rank, token, slot) of the pairs of every expert, in the order of its rows: by source rank, then token."""
+    pairs = {}
+    for s in range(wl.n_ranks):
+        for t in range(int(inp.num_tokens[s])):
+            for k in range(wl.top_k):
+                pairs.setdefault(int(inp.indices[s, t, k]), []).append((s, t, k))
+    return pairs
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("stream_ordered", [False, True])
+def test_a_layer_of_bf16_tokens(stream_ordered):
+    """dispatch, gated block, product, combine against the layer's formula in 64 bits, from the tokens to the sums."""
+    wl, inp, dev, harness = layer_inputs()
+    inter = 136
+    sh = harness.make_shuffle(inp, stream_ordered=stream_ordered, expert_align=16)
+    ex, (w, v) = harness.make_experts(sh, inter)
+    out = harness.run_layer(sh, ex, (w, v), dev).clone()
+    assert sh.status() == 0
+    x = dev["x"].double()
+    want, off = torch.zeros(out.shape, dtype=torch.float64, device="cuda"), torch.zeros(out.shape, dtype=torch.float64, device="cuda")
+    for e, pairs in tokens_by_expert(wl, inp).items():
+        s, t, k = (torch.tensor(c, device="cuda") for c in zip(*pairs))
+        _, _, h, dh = gated64(x[s, t], w[e].double(), 0)
+        dh = h.abs() * BF16 + (1 + BF16) * dh                # h is rounded to bf16
+        y, size = h @ v[e].double().T, (h.abs() + dh) @ v[e].double().abs().T
+        dy = dh @ v[e].double().abs().T + inter * U * size
+        dy = y.abs() * BF16 + (1 + BF16) * dy                # and y
+        g = dev["weights"][s, t, k].double()[:, None]
+        want.index_put_((s, t), g * y, accumulate=True)
+        off.index_put_((s, t), g.abs() * (dy + wl.top_k * U * (y.abs() + dy)), accumulate=True)
+    for r in range(wl.n_ranks):
+        n = int(inp.num_tokens[r])
+        check(out[r, :n], want[r, :n], want[r, :n].abs() * BF16 + (1 + BF16) * off[r, :n] + TINY, f"out of rank {r}")
+    sh.close()
+
+
+@pytest.mark.gpu
+def test_a_layer_of_e4m3_tokens():
+    """The same with e4m3 dispatch: the rows are the oracle-checked codes, so the products are held against them."""
+    wl, inp, dev, harness = layer_inputs(dispatch_dtype="e4m3")
+    inter = 128
+    sh = harness.make_shuffle(inp)
+    ex, (w, v, ws, vs) = harness.make_experts(sh, inter)
+    out = harness.run_layer(sh, ex, (w, v, ws, vs), dev)
+    assert sh.status() == 0
+    tabs = sh.layout_tables()
+    wide = lambda c, s: c.float().double() * s.double().repeat_interleave(128, 1)[:, :c.shape[1]].repeat_interleave(128, 2)
+    w64, v64 = wide(w, ws), wide(v, vs)
+    x64 = dequantised(sh.expert_x.view(torch.float8_e4m3fn), sh.expert_scales)
+    h64 = dequantised(ex.h.view(torch.float8_e4m3fn), ex.h_scales)
+    for d in range(wl.n_ranks):
+        for j in range(sh.El):
+            lo, n, e = int(tabs["expert_off"][d, j]), int(tabs["G"][d, j]), d * sh.El + j
+            rows = slice(lo, lo + n)
+            _, _, h, dh = gated64(x64[d, rows], w64[e], 0, sums(wl.hidden), cut(x64[d, rows], w64[e]))
+            s = ex.h_scales[d, rows].double().repeat_interleave(128, 1)
+            check(h64[d, rows], h, (h.abs() + dh) * 2.0 ** -4 * (1 + 8 * U) + s * 2.0 ** -10 + dh + h.abs() * 4 * U + TINY, f"h of {e}")
+            y = h64[d, rows] @ v64[e].T
+            dy = sums(inter) * U * (h64[d, rows].abs() @ v64[e].abs().T) + cut(h64[d, rows], v64[e])
+            check(ex.y[d, rows], y, y.abs() * BF16 + (1 + BF16) * dy + TINY, f"y of {e}")
+    for r in range(wl.n_ranks):
+        assert bool(out[r, :int(inp.num_tokens[r])].isfinite().all())
+    sh.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("keep", ["bf16", "e4m3"])
+def test_a_training_step_of_a_layer(keep):
+    """Forward, another layer's step in between, backward: every gradient against the formula on what the layer kept, from
+    the sums' gradient to the tokens'."""
+    wl, inp, dev, harness = layer_inputs()
+    inter = 128
+    sh = harness.make_shuffle(inp)
+    ex, (w, v) = harness.make_experts(sh, inter, training=True, keep=keep)
+    harness.run_layer(sh, ex, (w, v), dev)
+    x = sh.expert_x.clone()
+    off, load = (t.cpu() for t in ex.tables)
+    kept = ex.pre.clone()
+    kept64 = dequantised(kept.view(torch.float8_e4m3fn), ex.pre_scales) if keep == "e4m3" else kept.double()
+    other = dict(dev, indices=(dev["indices"] + 5) % wl.n_experts)
+    pairs = tokens_by_expert(wl, inp)
+    row_weights = torch.zeros((sh.N, sh.expert_capacity_rows), device="cuda")
+    for e, p in pairs.items():
+        d, j = e // sh.El, e % sh.El
+        s, t, k = (torch.tensor(c, device="cuda") for c in zip(*p))
+        row_weights[d, int(off[d, j]):int(off[d, j]) + len(p)] = dev["weights"][s, t, k]
+        assert len(p) == int(load[d, j])
+    harness.run_step(sh, other)              # another layer, with other routing, uses the same shuffle
+    g = torch.Generator(device="cuda").manual_seed(1)
+    dout = torch.randn(sh.out.shape, generator=g, device="cuda").to(torch.bfloat16)
+    dw, dv = torch.full_like(w, 77), torch.full_like(v, 77)
+    dx = harness.run_layer_backward(sh, ex, (w, v), (dw, dv), dev, x, dout, row_weights, torch.ones_like(dev["weights"]))
+    assert sh.status() == 0
+    dy64 = torch.zeros(x.shape, dtype=torch.float64, device="cuda")
+    for e, p in pairs.items():
+        d, j = e // sh.El, e % sh.El
+        s, t, k = (torch.tensor(c, device="cuda") for c in zip(*p))
+        dy64[d, int(off[d, j]):int(off[d, j]) + len(p)] = (dout[s, t].float() * dev["weights"][s, t, k][:, None]).to(torch.bfloat16).double()
+    for e in range(wl.n_experts):
+        d, j = e // sh.El, e % sh.El
+        n = int(load[d, j])
+        rows = slice(int(off[d, j]), int(off[d, j]) + n)
+        xe, dy, p = x[d, rows].double(), dy64[d, rows], kept64[d, rows]
+        a, slope, _ = act64(p[:, :inter], 0)
+        h = ex.h[d, rows].double()
+        bound = lambda want, size, steps: want.abs() * BF16 + (1 + BF16) * steps * U * size + TINY
+        if keep == "e4m3":
+            check(h, a * p[:, inter:], (a * p[:, inter:]).abs() * (BF16 + 64 * U) + TINY, f"h again of {e}")
+        check(dv[e], dy.T @ h, bound(dy.T @ h, dy.abs().T @ h.abs(), n), f"dw_out of {e}")
+        dh = ex.dh[d, rows].double()
+        check(dh, dy @ v[e].double(), bound(dy @ v[e].double(), dy.abs() @ v[e].double().abs(), wl.hidden), f"dh of {e}")
+        dp = ex.dpre[d, rows].double()
+        want = torch.cat((dh * p[:, inter:] * slope, dh * a), 1)
+        check(dp, want, want.abs() * BF16 + (dh.abs() * (1 + p[:, inter:].abs())).repeat(1, 2) * U * 128 + TINY, f"dpre of {e}")
+        check(dw[e], dp.T @ xe, bound(dp.T @ xe, dp.abs().T @ xe.abs(), n), f"dw_in of {e}")
+        check(ex.dx[d, rows], dp @ w[e].double(), bound(dp @ w[e].double(), dp.abs() @ w[e].double().abs(), 2 * inter), f"dx of {e}")
+    # the tokens' gradient: sums over a token's rows of dx, in fp32 in the order of k, rounded once
+    sums_of = torch.zeros(dx.shape, dtype=torch.float64, device="cuda")
+    size = torch.zeros_like(sums_of)
+    for e, p in pairs.items():
+        d, j = e // sh.El, e % sh.El
+        s, t, k = (torch.tensor(c, device="cuda") for c in zip(*p))
+        r = ex.dx[d, int(off[d, j]):int(off[d, j]) + len(p)].double()
+        sums_of.index_put_((s, t), r, accumulate=True)
+        size.index_put_((s, t), r.abs(), accumulate=True)
+    for r in range(wl.n_ranks):
+        n = int(inp.num_tokens[r])
+        check(dx[r, :n], sums_of[r, :n], sums_of[r, :n].abs() * BF16 + (1 + BF16) * wl.top_k * U * size[r, :n] + TINY, f"dx of rank {r}")
+    sh.close()
+
+
+@pytest.mark.gpu
+def test_rows_of_e4m3_have_no_backward_pass():
+    wl, inp, dev, harness = layer_inputs(dispatch_dtype="e4m3")
+    sh = harness.make_shuffle(inp)
+    with pytest.raises(flmoe.FlMoeError):
+        flmoe.MoEExperts(sh, 128, training=True)
+    with pytest.raises(flmoe.FlMoeError):
+        flmoe.MoEExperts(sh, 128, keep="fp8")
+    sh.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("counts", [[[300, 70, 5]], [[64, 65], [33, 31]], [[1, 900]]])
+@pytest.mark.parametrize("tokens", [1, 30, 100000])
+def test_tiles_chosen_for_other_numbers_of_rows_are_right_too(tokens, counts):
+    """The tile goes by the mean that the configuration expects: few rows where many were meant, and the other way round."""
+    hidden, inter = 384, 256
+    L = Layer(counts, hidden)
+    cap = L.cap
+    L.cfg.max_tokens, L.cfg.top_k = max(tokens * L.el, 1), 1
+    sizes = flmoe.fl_moe_query_sizes(L.cfg)
+    if sizes.expert_capacity_rows != cap:                    # the configuration holds fewer rows than these tensors
+        L = Layer([[min(c, tokens) for c in per] for per in counts], hidden, cap=sizes.expert_capacity_rows)
+        L.cfg.max_tokens, L.cfg.top_k = max(tokens * L.el, 1), 1
+    at = (L.cfg, 0, L.n, L.expert_off, L.loads)
+    x, w, h = L.rows(hidden), L.weights(2 * inter, hidden), L.unwritten(inter)
+    v, y = L.weights(hidden, inter), L.unwritten(hidden)
+    (x8, xs), (w8, ws, w64) = e4m3_rows(L, hidden), e4m3_weights(L, 2 * inter, hidden)
+    h8, hs = L.unwritten(inter, torch.uint8).view(torch.float8_e4m3fn), L.unwritten(inter // 128, torch.float32)
+    pre, ps = L.unwritten(2 * inter, torch.uint8).view(torch.float8_e4m3fn), L.unwritten(2 * inter // 128, torch.float32)
+    h2 = L.unwritten(inter)
+    flmoe.fl_moe_expert_gated(*at, inter, 0, x, w, h)
+    flmoe.fl_moe_expert_gated(*at, inter, 0, x, w, h2, pre, ps)
+    assert torch.equal(h, h2)
+    flmoe.fl_moe_expert_product(*at, inter, hidden, h, v, y)
+    flmoe.fl_moe_expert_gated_e4m3(*at, inter, 0, x8, xs, w8, ws, h8, hs)
+    want, tol, ywant, ytol, want8, off8, kept, kept_off = ({} for _ in range(8))
+    for d, j in L.experts():
+        rows, e = L.span(d, j), d * L.el + j
+        p, dp, h64, dh = gated64(x[d, rows].double(), w[e].double(), 0)
+        want[d, j], tol[d, j] = h64, h64.abs() * BF16 + (1 + BF16) * dh + TINY
+        kept[d, j], kept_off[d, j] = p, dp
+        he = h[d, rows].double()
+        ywant[d, j] = he @ v[e].double().T
+        ytol[d, j] = ywant[d, j].abs() * BF16 + (1 + BF16) * inter * U * (he.abs() @ v[e].double().abs().T) + TINY
+        x64 = dequantised(x8[d, rows], xs[d, rows])
+        _, _, want8[d, j], off8[d, j] = gated64(x64, w64[e], 0, sums(hidden), cut(x64, w64[e]))
+    L.check_rows(h, want, tol, "h")
+    L.check_rows(y, ywant, ytol, "y")
+    check_blocks(L, h8, hs, want8, off8, "h in e4m3")
+    check_blocks(L, pre, ps, kept, kept_off, "pre in e4m3")
