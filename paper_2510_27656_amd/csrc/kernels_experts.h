@@ -454,30 +454,42 @@ struct Tile {
             read_b(fb0[0], 0);
             loads_done_and_barrier<kAhead>();
             load(B0, 2, t); load_scales(2, t); load(A0, 2, t);
-            auto body = [&](int step, auto parity) FLMOE_INLINE {
+            // full: whether this wave has rows in B1 as well
+            auto body = [&](int step, auto parity, auto full) FLMOE_INLINE {
                 constexpr int s = parity();
+                constexpr bool both = full();
                 constexpr int a_here = s * 2 * kUnitA, a_next = (1 - s) * 2 * kUnitA, b_here = s * 2 * kUnitB, b_next = (1 - s) * 2 * kUnitB;
                 scales_of_weights(step, parity, t);
                 scales_of(step, 0);
-                read_b(fb1, b_here + kUnitB);
-                in_order();
-                multiply(Zero(), Zero(), fb0[s], w[0], nothing);
-                scales_of(step, 1);
-                multiply_and_read_a(Zero(), One(), fb1, w[0], a_here + kUnitA);
+                if constexpr (both) {
+                    read_b(fb1, b_here + kUnitB);
+                    in_order();
+                    multiply(Zero(), Zero(), fb0[s], w[0], nothing);
+                    scales_of(step, 1);
+                    multiply_and_read_a(Zero(), One(), fb1, w[0], a_here + kUnitA);
+                } else {
+                    multiply_and_read_a(Zero(), Zero(), fb0[s], w[0], a_here + kUnitA);
+                }
                 loads_done_and_barrier<kAhead>();
                 load(B1, step + 2, t); load(A1, step + 2, t);
                 read_b(fb0[1 - s], b_next);
                 in_order();
-                multiply(One(), One(), fb1, w[1], nothing);
-                scales_of(step, 0);
+                if constexpr (both) {
+                    multiply(One(), One(), fb1, w[1], nothing);
+                    scales_of(step, 0);
+                }
                 multiply_and_read_a(One(), Zero(), fb0[s], w[1], a_next);
                 loads_done_and_barrier<kAhead>();
                 load(B0, step + 3, t); load_scales(step + 3, t); load(A0, step + 3, t);
             };
-            for (int step = 0; step < steps; step += 2) {              // behind an odd last step, one of zeros
-                body(step, Zero());
-                body(step + 1, One());
-            }
+            auto all = [&](auto full) FLMOE_INLINE {
+                for (int step = 0; step < steps; step += 2) {          // behind an odd last step, one of zeros
+                    body(step, Zero(), full);
+                    body(step + 1, One(), full);
+                }
+            };
+            if (kUnitRows + wr * kOwnR < n_b - tile.r0) all(One());
+            else all(Zero());
         };
         auto one_unit = [&]() FLMOE_INLINE {
             // No B1, two phases: A0 B0 while A1 is read over A0, then A1 B0 while the next step's A0 and B0 are read.  Waves
@@ -685,17 +697,25 @@ struct Tile {
     }
 };
 
-// Row tiles of the call's experts before each, in LDS: [n + 1].
-template <int THREADS>
-__device__ inline void scan_tiles(const Groups &G, int rows_per_tile, int *before) {
+// What the workgroups share out, in LDS.  Row tiles, or cost, of the call's experts before each: [n + 1]; and the experts
+// whose last, short row tile comes behind all others.
+struct Shares {
+    int before[kMaxExperts + 1];
+    unsigned long long short_tile[kMaxExperts / 64];
+};
+// value(rows of an expert, &whether it has a tile of the second kind): what is summed.
+template <int THREADS, class Value>
+__device__ inline void scan(const Groups &G, Shares &S, Value value) {
     __shared__ int part[THREADS / kWave];
-    constexpr int kThreads = THREADS, kWaves = THREADS / kWave;
     const int tid = threadIdx.x, lane = tid & (kWave - 1);
     int carry = 0;
-    if (tid == 0) before[0] = 0;
-    for (int base = 0; base < G.n; base += kThreads) {
+    if (tid == 0) S.before[0] = 0;
+    for (int base = 0; base < G.n; base += THREADS) {
         int v = 0;
-        if (base + tid < G.n) v = (int)(((long long)rows_of(G, G.first + base + tid).n + rows_per_tile - 1) / rows_per_tile);
+        bool second = false;
+        if (base + tid < G.n) v = value(rows_of(G, G.first + base + tid).n, &second);
+        const unsigned long long seconds = __ballot(second);
+        if (lane == 0 && base + tid < kMaxExperts) S.short_tile[(base + tid) / 64] = seconds;
 #pragma unroll
         for (int o = 1; o < kWave; o <<= 1) {
             const int w = __shfl_up(v, o);
@@ -704,53 +724,111 @@ __device__ inline void scan_tiles(const Groups &G, int rows_per_tile, int *befor
         if (lane == kWave - 1) part[tid / kWave] = v;
         __syncthreads();
         int mine = carry;
-        for (int w = 0; w < kWaves; ++w) {
+        for (int w = 0; w < THREADS / kWave; ++w) {
             if (w < tid / kWave) mine += part[w];
             carry += part[w];
         }
-        if (base + tid < G.n) before[base + tid + 1] = mine + v;
+        if (base + tid < G.n) S.before[base + tid + 1] = mine + v;
         __syncthreads();
     }
 }
+// Largest i < n with before[i] <= x.
+__device__ inline int expert_at(const Shares &S, int n, int x) {
+    int lo = 0, hi = n;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (S.before[mid] <= x) lo = mid; else hi = mid;
+    }
+    return lo;
+}
 
 constexpr int kRowGroup = 8;                   // row tiles that walk the features together
+// An expert of this many row tiles has a last one of at most half the rows behind all others, so that what is left for the last
+// turns is short as well; with fewer, whoever reads the weights for the others had better have it, too.
+constexpr int kTilesBeforeShort = 4;
+constexpr int kTileCost = 8;                   // weight gradient: what begins and ends a tile, in steps of the contraction
 
 template <int FORM, bool E4M3, bool GATED, int ROWS, int HALF>
 __global__ __launch_bounds__((Tile<FORM, E4M3, GATED, ROWS, HALF>::kThreads), 2) void expert_tiles_kernel(Groups G, Product P) {
     using T = Tile<FORM, E4M3, GATED, ROWS, HALF>;
+    constexpr bool kWeights = FORM == kWeightGradient;
     __shared__ __align__(1024) char lds[T::kLds];
-    __shared__ int before[kMaxExperts + 1];
+    __shared__ Shares S;
     const int columns = (P.features + T::kOutput - 1) / T::kOutput;
-    const int fixed = FORM == kWeightGradient ? (P.other + ROWS - 1) / ROWS : 0;
-    if (FORM != kWeightGradient) scan_tiles<T::kThreads>(G, ROWS, before);
-    const long long tiles = (long long)(FORM == kWeightGradient ? G.n * fixed : before[G.n]) * columns;
-    // Workgroups go to the XCDs in turn.  Each XCD has an eighth of the tiles, neighbours, whose operands its L2 then holds.
+    // Workgroups go to the XCDs in turn.  Each XCD has a share of the tiles, neighbours, whose operands its L2 then holds, and its
+    // workgroups take them in turn.
     const int xcd = blockIdx.x % kXcds;
-    const long long end = tiles * (xcd + 1) / kXcds;
-    long long t = tiles * xcd / kXcds + blockIdx.x / kXcds;
+    long long first, whole, first_short = 0, all;      // this XCD's: first tile, number of them, first short one, number of both
+    int per_expert = 0;                                // weight gradient: tiles
+    if constexpr (kWeights) {
+        per_expert = (P.other + ROWS - 1) / ROWS * columns;
+        scan<T::kThreads>(G, S, [](int n, bool *) { return (n < 1 << 26 ? (n + 63) / 64 : 1 << 20) + kTileCost; });
+        // Shares of equal cost, experts' contractions differ (128 experts of 1 to 1694 rows 464 -> 425 us), begun at whole turns of an
+        // XCD's workgroups, since a part of a turn takes as long as a whole one (shares to the tile: 64 experts of 2048 rows
+        // 481 -> 496). One grid for all starts keeps them in order. Less than a turn for each: equal numbers.
+        auto start = [&](int x) -> long long {
+            const long long tiles = (long long)G.n * per_expert, turn = gridDim.x / kXcds;
+            if (x == 0 || x == kXcds || tiles < kXcds * turn) return tiles * x / kXcds;
+            const long long cost = (long long)S.before[G.n] * x / kXcds;
+            const int e = expert_at(S, G.n, (int)cost);
+            const long long at = (long long)e * per_expert + (cost - S.before[e]) * per_expert / (S.before[e + 1] - S.before[e]);
+            const long long even = (at + turn / 2) / turn * turn;
+            return even < tiles ? even : tiles;
+        };
+        first = start(xcd);
+        all = whole = start(xcd + 1) - first;
+    } else {
+        scan<T::kThreads>(G, S, [](int n, bool *second) {
+            *second = ROWS == 256 && n / ROWS >= kTilesBeforeShort && n % ROWS && n % ROWS <= ROWS / 2;
+            return n / ROWS + (n % ROWS && !*second);
+        });
+        const long long tiles = (long long)S.before[G.n] * columns;
+        first = tiles * xcd / kXcds;
+        all = whole = tiles * (xcd + 1) / kXcds - first;
+        if (ROWS == 256) {
+            int n = 0;
+            for (int w = 0; w * 64 < G.n; ++w) n += __popcll(S.short_tile[w]);
+            const long long shorts = (long long)n * columns;
+            first_short = shorts * xcd / kXcds;
+            all += shorts * (xcd + 1) / kXcds - first_short;
+        }
+    }
+    long long t = blockIdx.x / kXcds;
     T::run(P, lds, [&](typename T::Place *to) {
-        for (; t < end; t += gridDim.x / kXcds) {
-            const int row_tile = (int)(t / columns);                   // counted over the experts
-            int lo = 0, hi = G.n, n_tiles, index;
-            if constexpr (FORM == kWeightGradient) {
-                lo = row_tile / fixed;
-                n_tiles = fixed;
-                index = (int)(t - (long long)lo * fixed * columns);
-            } else {
-                while (hi - lo > 1) {
-                    const int mid = (lo + hi) >> 1;
-                    if (before[mid] <= row_tile) lo = mid; else hi = mid;
+        for (; t < all; t += gridDim.x / kXcds) {
+            int lo, column, row;                       // expert, column of tiles, row of tiles
+            if (t < whole) {
+                const long long tile = first + t;
+                int n_tiles, index;
+                if constexpr (kWeights) {
+                    lo = (int)(tile / per_expert);
+                    n_tiles = per_expert / columns;
+                    index = (int)(tile - (long long)lo * per_expert);
+                } else {
+                    lo = expert_at(S, G.n, (int)(tile / columns));
+                    n_tiles = S.before[lo + 1] - S.before[lo];
+                    index = (int)(tile - (long long)S.before[lo] * columns);
                 }
-                n_tiles = before[lo + 1] - before[lo];
-                index = (int)(t - (long long)before[lo] * columns);
+                const int group = index / (kRowGroup * columns), left = n_tiles - group * kRowGroup;
+                const int in_group = left < kRowGroup ? left : kRowGroup, within = index - group * kRowGroup * columns;
+                column = within / in_group;
+                row = group * kRowGroup + within - column * in_group;
+            } else {
+                const long long tile = first_short + t - whole;
+                int nth = (int)(tile / columns), w = 0;
+                column = (int)(tile - (long long)nth * columns);
+                unsigned long long have = S.short_tile[0];
+                for (int n; nth >= (n = __popcll(have)) && (w + 1) * 64 < G.n; have = S.short_tile[++w]) nth -= n;
+                for (; nth > 0; --nth) have &= have - 1;
+                lo = w * 64 + __ffsll(have) - 1;
+                row = -1;
             }
-            const int group = index / (kRowGroup * columns), left = n_tiles - group * kRowGroup;
-            const int in_group = left < kRowGroup ? left : kRowGroup, within = index - group * kRowGroup * columns;
-            const int column = within / in_group, row = group * kRowGroup + within - column * in_group;
+            if (lo < 0) continue;
             const int e = G.first + __builtin_amdgcn_readfirstlane(lo);
             const Rows found = rows_of(G, e), rows = {same_in_wave(found.first), __builtin_amdgcn_readfirstlane(found.n)};
+            if (row < 0) row = rows.n / ROWS;
             // (tables that claim more rows than there can be may have wrapped the sums)
-            if ((unsigned)column >= (unsigned)columns || row < 0 || (long long)row * ROWS >= (FORM == kWeightGradient ? P.other : rows.n)) continue;
+            if ((unsigned)column >= (unsigned)columns || row < 0 || (long long)row * ROWS >= (kWeights ? P.other : rows.n)) continue;
             *to = {e, rows, __builtin_amdgcn_readfirstlane(column) * T::kOutput, __builtin_amdgcn_readfirstlane(row) * ROWS};
             t += gridDim.x / kXcds;
             return true;

@@ -806,3 +806,40 @@ def test_tiles_chosen_for_other_numbers_of_rows_are_right_too(tokens, counts):
     L.check_rows(y, ywant, ytol, "y")
     check_blocks(L, h8, hs, want8, off8, "h in e4m3")
     check_blocks(L, pre, ps, kept, kept_off, "pre in e4m3")
+
+
+# experts of some whole tiles of rows and a rest, among many of few rows or none; one of nearly all rows
+UNEVEN = [
+    [[(1024 + rest if j % 5 == 0 else j % 4) for j in range(70) for rest in ((1, 64, 128, 129, 255, 256, 0)[j // 5 % 7],)]],
+    [[0] * 40 + [1152] + [1] * 4, [0] * 44 + [1281], [2] * 44 + [1300]],
+    [[5000] + [0] * 62 + [1, 7]],
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("counts", UNEVEN)
+def test_tiles_of_uneven_experts_are_each_done_once(counts):
+    """More tiles than workgroups and shares that differ: the last tiles of long experts come behind all others, and the weight
+    gradients' shares go by the experts' rows."""
+    in_, out = 512, 776
+    L = Layer(counts, in_)
+    x, w, dy = L.rows(in_), L.weights(out, in_), L.rows(out)
+    y, dx, dw = L.unwritten(out), L.unwritten(in_), torch.full_like(w, 77)
+    (x8, xs), (w8, ws, w64) = e4m3_rows(L, in_), e4m3_weights(L, out, in_)
+    y8 = L.unwritten(out)
+    flmoe.fl_moe_expert_product(*L.at, in_, out, x, w, y)
+    flmoe.fl_moe_expert_product_backward(*L.at, in_, out, x, w, dy, dx, dw)
+    flmoe.fl_moe_expert_product_e4m3(*L.at, in_, out, x8.view(torch.uint8), xs, w8, ws, y8)
+    want, tol = {"y": {}, "dx": {}, "y8": {}}, {"y": {}, "dx": {}, "y8": {}}
+    for d, j in L.experts():
+        rows, e = L.span(d, j), d * L.el + j
+        xe, we, de = x[d, rows].double(), w[e].double(), dy[d, rows].double()
+        want["y"][d, j], want["dx"][d, j] = xe @ we.T, de @ we
+        tol["y"][d, j] = want["y"][d, j].abs() * BF16 + (1 + BF16) * in_ * U * (xe.abs() @ we.abs().T) + TINY
+        tol["dx"][d, j] = want["dx"][d, j].abs() * BF16 + (1 + BF16) * out * U * (de.abs() @ we.abs()) + TINY
+        check(dw[e], de.T @ xe, (de.T @ xe).abs() * BF16 + (1 + BF16) * L.counts[d][j] * U * (de.abs().T @ xe.abs()) + TINY, f"dw of expert {e}")
+        x64, we = dequantised(x8[d, rows], xs[d, rows]), w64[e]
+        want["y8"][d, j] = x64 @ we.T
+        tol["y8"][d, j] = want["y8"][d, j].abs() * BF16 + (1 + BF16) * (sums(in_) * U * (x64.abs() @ we.abs().T) + cut(x64, we)) + TINY
+    for name, got in (("y", y), ("dx", dx), ("y8", y8)):
+        L.check_rows(got, want[name], tol[name], name)
