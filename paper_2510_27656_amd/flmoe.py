@@ -606,28 +606,31 @@ class MoEExperts:
             # the pre-activations' gradients take the place of what was kept where they fit
             self.dpre = rows(2 * inter) if eights else self.pre
             self.dh, self.dx = rows(inter), rows(shuffle.H)
+            self.tables = [torch.zeros((shuffle.N, n), dtype=torch.int32, device=shuffle.device) for n in (shuffle.El + 1, shuffle.El)]
 
     def _at(self, ranks):
         rb, rc = self.shuffle._ranks(ranks)
         return (self.shuffle.cfg, rb, rc, *self.tables)
 
-    def forward(self, w_in, w_out, in_scales=None, out_scales=None, x=None, ranks=None, stream=None):
-        """y of the rows that dispatch_recv left (x: of other rows in that layout)."""
+    def forward(self, w_in, w_out, in_scales=None, out_scales=None, x=None, ranks=None, stream=None, x_scales=None):
+        """y of the rows that dispatch_recv left (x, and of e4m3 rows x_scales: of other rows in that layout)."""
         sh = self.shuffle
+        if (x_scales is not None) != (x is not None and self.e4m3):
+            raise FlMoeError(FL_ERR_INVALID_ARG, "MoEExperts.forward: other rows of e4m3 come with their scales")
         if self.training:
             on = torch.cuda.current_stream(sh.device) if stream is None else stream
+            if not hasattr(on, "cuda_stream"):
+                on = torch.cuda.ExternalStream(int(on), device=sh.device)
             with torch.cuda.stream(on):
-                tabs = sh.layout_tables()
-                if self.tables is None:
-                    self.tables = [torch.empty_like(tabs["expert_off"]), torch.empty_like(tabs["G"])]
-                self.tables[0].copy_(tabs["expert_off"])
-                self.tables[1].copy_(tabs["G"])
+                rb, rc = sh._ranks(ranks)                # only theirs: the others' may be on their way on other streams
+                for mine, now in zip(self.tables, (sh.layout_tables()[t] for t in ("expert_off", "G"))):
+                    mine[rb:rb + rc].copy_(now[rb:rb + rc])
         else:
             self.tables = (sh.view.expert_off, sh.view.tokens_per_expert)
         at, x = self._at(ranks), sh.expert_x if x is None else x
         if self.e4m3:
-            fl_moe_expert_gated_e4m3(*at, self.inter, self.activation, x, sh.expert_scales, w_in, in_scales, self.h,
-                                     self.h_scales, stream)
+            fl_moe_expert_gated_e4m3(*at, self.inter, self.activation, x, sh.expert_scales if x_scales is None else x_scales,
+                                     w_in, in_scales, self.h, self.h_scales, stream)
             fl_moe_expert_product_e4m3(*at, self.inter, sh.H, self.h, self.h_scales, w_out, out_scales, self.y, stream)
         else:
             fl_moe_expert_gated(*at, self.inter, self.activation, x, w_in, self.h, self.pre, self.pre_scales, stream)
@@ -637,6 +640,8 @@ class MoEExperts:
     def backward(self, dy, w_in, w_out, dw_in, dw_out, x=None, ranks=None, stream=None):
         """The rows' gradient; the weights' go to dw_in and dw_out.  Once per forward: with bf16 the kept pre-activations are
         gone then.  x: the rows that forward had."""
+        if not self.training:
+            raise FlMoeError(FL_ERR_INVALID_ARG, "MoEExperts.backward: nothing was kept, training was not asked for")
         sh, at = self.shuffle, self._at(ranks)
         x = sh.expert_x if x is None else x
         again = self.h if self.keep == "e4m3" else None

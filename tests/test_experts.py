@@ -843,3 +843,61 @@ def test_tiles_of_uneven_experts_are_each_done_once(counts):
         tol["y8"][d, j] = want["y8"][d, j].abs() * BF16 + (1 + BF16) * (sums(in_) * U * (x64.abs() @ we.abs().T) + cut(x64, we)) + TINY
     for name, got in (("y", y), ("dx", dx), ("y8", y8)):
         L.check_rows(got, want[name], tol[name], name)
+
+
+@pytest.mark.gpu
+def test_a_layer_rank_by_rank_keeps_each_ranks_own_tables():
+    """As a real rank calls it, streams given as handles: the others' tables, which may be in the making, are left alone."""
+    wl, inp, dev, harness = layer_inputs()
+    sh = harness.make_shuffle(inp)
+    ex, (w, v) = harness.make_experts(sh, 128, training=True)
+    harness.run_layer(sh, ex, (w, v), dev)
+    y, tables = ex.y.clone(), [t.clone() for t in ex.tables]
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    for r in range(wl.n_ranks):
+        ex.y.fill_(77)
+        for t in ex.tables:
+            t.fill_(-5)
+        stream.wait_stream(torch.cuda.current_stream())
+        ex.forward(w, v, ranks=(r, 1), stream=stream.cuda_stream)
+        stream.synchronize()
+        for d in range(wl.n_ranks):
+            for mine, whole in zip(ex.tables, tables):
+                assert torch.equal(mine[d], whole[d] if d == r else torch.full_like(whole[d], -5))
+            for j in range(sh.El):
+                rows = slice(int(tables[0][d, j]), int(tables[0][d, j] + tables[1][d, j]))
+                assert torch.equal(ex.y[d, rows], y[d, rows] if d == r else torch.full_like(y[d, rows], 77))
+    sh.close()
+
+
+@pytest.mark.gpu
+def test_other_rows_of_e4m3_come_with_their_scales():
+    wl, inp, dev, harness = layer_inputs(dispatch_dtype="e4m3")
+    sh = harness.make_shuffle(inp)
+    ex, weights = harness.make_experts(sh, 128)
+    harness.run_layer(sh, ex, weights, dev)
+    y, x, scales = ex.y.clone(), sh.expert_x.clone(), sh.expert_scales.clone()
+    harness.run_step(sh, dev)
+    sh.expert_x.fill_(0x7f)
+    for given in (dict(x=x), dict(x_scales=scales)):
+        with pytest.raises(flmoe.FlMoeError):
+            ex.forward(*weights, **given)
+    off, load = (sh.layout_tables()[t].cpu() for t in ("expert_off", "G"))
+    again = ex.forward(*weights, x=x, x_scales=scales)
+    for d in range(wl.n_ranks):
+        for j in range(sh.El):
+            rows = slice(int(off[d, j]), int(off[d, j] + load[d, j]))
+            assert torch.equal(again[d, rows], y[d, rows])
+    sh.close()
+
+
+@pytest.mark.gpu
+def test_no_backward_pass_of_what_was_not_kept():
+    wl, inp, dev, harness = layer_inputs()
+    sh = harness.make_shuffle(inp)
+    ex, (w, v) = harness.make_experts(sh, 128)
+    harness.run_layer(sh, ex, (w, v), dev)
+    with pytest.raises(flmoe.FlMoeError):
+        ex.backward(ex.y, w, v, torch.empty_like(w), torch.empty_like(v))
+    sh.close()
