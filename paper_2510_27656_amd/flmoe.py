@@ -85,7 +85,8 @@ EXPORTS = ["fl_moe_query_sizes", "fl_moe_create", "fl_moe_destroy", "fl_moe_layo
            "fl_moe_dispatch_recv",
            "fl_moe_combine_send",
            "fl_moe_combine_reduce", "fl_moe_expert_gated", "fl_moe_expert_gated_backward", "fl_moe_expert_product",
-           "fl_moe_expert_product_backward", "fl_moe_expert_gated_e4m3", "fl_moe_expert_product_e4m3", "fl_moe_status", "fl_moe_reset", "fl_moe_required_capacities",
+           "fl_moe_expert_product_backward", "fl_moe_expert_gated_e4m3", "fl_moe_expert_product_e4m3",
+           "fl_moe_status", "fl_moe_reset", "fl_moe_required_capacities",
            "fl_moe_strerror", "fl_moe_debug_views", "fl_moe_debug_row_strides",
            "fl_moe_debug_tune", "fl_moe_debug_launch_groups", "fl_moe_debug_launch_plan", "fl_moe_debug_ordering_plan",
            "fl_moe_debug_copy", "fl_moe_debug_fill", "fl_moe_debug_read", "fl_moe_profile_enable", "fl_moe_profile_collect", "fl_moe_profile_read",
