@@ -154,8 +154,8 @@ __device__ inline void loads_done_and_barrier() {
 // A phase ends with: this wave's reads are done, its loads for the next phase's units have arrived, barrier; then the
 // units just read are loaded for two steps later.  So with two places for each unit the loads that fill one have a step
 // and a half to arrive, and 64 to 96 KB are on their way to a compute unit all the time.  (Four phases of one quadrant
-// each: row gradient of 32 x 1024 rows of 7168 x 2048 454 us, so 428.)
-// Dense and full, bf16 reaches 1340 Tflop/s (a large library product on this card 1400 to 1600), e4m3 2010: there the block
+// each, a barrier behind each: the row gradient took 6 % longer.)
+// Dense and full, bf16 reaches 1340 to 1470 Tflop/s (a large library product on this card 1400 to 1600), e4m3 2010 to 2140: there the block
 // scales' fused multiplications take about an eighth of the time and the loads into LDS a fifth.
 constexpr int kStep = 128;                     // bytes of the contraction per step
 constexpr int kXcds = 8;
@@ -589,10 +589,24 @@ struct Tile {
                     asm volatile("" ::: "memory");
                 }
         };
+        // Whole lines that the kernel does not read again go past the caches, which keep the operands: training step of 128 experts
+        // of 1 to 1694 rows 1035 -> 1019 us, both e4m3 products of 64 x 128 rows 668 -> 649, that of 32 x 250 rows of 1024 x 2048
+        // 28.0 -> 27.1.  Not rows that begin inside lines (2056 wide 42.7 -> 43.8), nor a gated block's output, which the next
+        // product reads.
+        const bool past = ROWS == 256 && !GATED && P.features % 64 == 0;
+        auto put = [&](auto w, char *to) {
+            if (past) {
+                asm volatile("");                              // (or the compiler makes one plain store of the two)
+                __builtin_nontemporal_store(w, (decltype(w) *)to);
+                asm volatile("");
+            } else {
+                *(decltype(w) *)to = w;
+            }
+        };
         // the eight features from f on of row `row` of a tensor `width` features wide
         auto put_bf16 = [&](void *to, size_t row, int f, int width, const float *v) {
             const v4u w = {to_bf16x2(v[0], v[1]), to_bf16x2(v[2], v[3]), to_bf16x2(v[4], v[5]), to_bf16x2(v[6], v[7])};
-            *(v4u *)((char *)to + (row * width + f) * 2) = w;
+            put(w, (char *)to + (row * width + f) * 2);
         };
         // in blocks of e4m3; the tile's 128 features are one block
         auto find_largest = [&](auto value) FLMOE_INLINE {
@@ -618,7 +632,7 @@ struct Tile {
             for (int i = 0; i < kWavesF; ++i) m = fmaxf(m, largest[i * ROWS + row]);
             const float scale = block_scale(m);
             const v2u w = {e4m3_codes(v, scale), e4m3_codes(v + 4, scale)};
-            *(v2u *)((char *)to + (row0 + row) * width + f) = w;
+            put(w, (char *)to + (row0 + row) * width + f);
             if (wf == 0 && (el & (kPieces - 1)) == 0) scales[(row0 + row) * (width / 128) + f / 128] = scale;
         };
         auto write = [&](const Place &done) FLMOE_INLINE {
