@@ -108,7 +108,9 @@ __device__ inline unsigned e4m3_codes(const float *v, float scale) {
 // read as zero; only offsets inside the tensor or kNowhere are ever passed, the limit is the largest there is.  Written
 // out because the compiler, which knows that these loads write LDS, lets every read of LDS behind them wait for them:
 // here the waits are the ones below, once per step.  Nothing is returned, so no register is written behind its back.
-// (One wait state lies between a write of m0 and a load that goes by it.)
+// One wait state lies between a write of m0 and a load that goes by it.  And five between a vector instruction that writes a
+// scalar register (also v_readlane, which brings back a spilled one) and the load that reads it: the compiler sees to that
+// before its own loads, not before inline assembly, so the first load here begins with them.
 #define FLMOE_LDS __attribute__((address_space(3)))
 constexpr unsigned kNowhere = 0x80000000u;
 struct Window {
@@ -120,12 +122,20 @@ struct Window {
 };
 __device__ inline unsigned lds_address(const char *lds) { return (unsigned)(uintptr_t)(FLMOE_LDS const char *)lds; }
 __device__ inline void to_lds_16(const Window &w, unsigned offset, unsigned shift, unsigned lds) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
-                 ::"s"(__builtin_amdgcn_readfirstlane((int)lds)), "v"(offset), "s"(w.rsrc), "s"(__builtin_amdgcn_readfirstlane((int)shift)) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                 ::"s"(__builtin_amdgcn_readfirstlane((int)lds)), "v"(offset), "s"(w.rsrc), "s"(__builtin_amdgcn_readfirstlane((int)shift)) : "memory", "m0");
+}
+// Two of them, DISTANCE bytes of LDS apart.
+template <int DISTANCE>
+__device__ inline void two_to_lds_16(const Window &w, unsigned offset, unsigned offset2, unsigned shift, unsigned lds) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %3, %4 offen lds\n\t"
+                 "s_add_u32 m0, m0, %5\n\ts_nop 0\n\tbuffer_load_dwordx4 %2, %3, %4 offen lds"
+                 ::"s"(__builtin_amdgcn_readfirstlane((int)lds)), "v"(offset), "v"(offset2), "s"(w.rsrc),
+                 "s"(__builtin_amdgcn_readfirstlane((int)shift)), "n"(DISTANCE) : "memory", "m0", "scc");
 }
 __device__ inline void to_lds_4(const Window &w, unsigned offset, unsigned shift, unsigned lds) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, %3 offen lds"
-                 ::"s"(__builtin_amdgcn_readfirstlane((int)lds)), "v"(offset), "s"(w.rsrc), "s"(__builtin_amdgcn_readfirstlane((int)shift)) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dword %1, %2, %3 offen lds"
+                 ::"s"(__builtin_amdgcn_readfirstlane((int)lds)), "v"(offset), "s"(w.rsrc), "s"(__builtin_amdgcn_readfirstlane((int)shift)) : "memory", "m0");
 }
 // The compiler keeps what comes before apart from what comes behind.
 __device__ inline void in_order() {
@@ -317,12 +327,13 @@ struct Tile {
             const char *base = o ? b0 : u ? a1 : a0;
             const Window from(trans ? base + (size_t)at_k * 64 * ld : base);
             const unsigned to = lds0 + place(unit, step & 1) + wave * 1024;
-            auto one = [&](int j) {
+            auto offset = [&](int j) {
                 const bool there = step < steps && (trans && j ? at_k * 64 + depth + 32 < k : at_k < steps_here[o]);
-                to_lds_16(from, there ? off[o][u * 2 + j] : kNowhere, trans ? 0 : at_k * kStep, to + j * kWaves * 1024);
+                return there ? off[o][u * 2 + j] : kNowhere;
             };
-            one(0);
-            if (!o || kLoadsB == 2) one(1);
+            const unsigned along = trans ? 0 : at_k * kStep;
+            if (!o || kLoadsB == 2) two_to_lds_16<kWaves * 1024>(from, offset(0), offset(1), along, to);
+            else to_lds_16(from, offset(0), along, to);
         };
         auto load_scales = [&](int step, auto turn) {
             if constexpr (E4M3) {

@@ -359,3 +359,61 @@ def test_nothing_overwrites_the_data_of_a_store_while_it_is_read(compiled):
 def test_loaded_library_was_built_from_the_sources_in_the_tree():
     from paper_2510_27656_amd import build
     assert flmoe.fl_moe_build_id() == build.source_hash() and len(build.source_hash()) == 16
+
+
+def early_scalar_reads(assembly, needed=5):
+    """Places where a vector memory instruction reads a scalar register fewer than `needed` wait states after a vector
+    instruction wrote it, along any path.  The compiler keeps them apart, but neither looks into inline assembly."""
+    def scalars(text):
+        regs = set()
+        for lo, hi, one in re.findall(r"\bs\[(\d+):(\d+)\]|\bs(\d+)\b", text):
+            regs.update(range(int(lo or one), int(hi or one) + 1))
+        return regs | ({"vcc"} if re.search(r"\bvcc\b", text) else set())
+    code = [line.split(";")[0].strip() for line in assembly.splitlines()]
+    code = [line for line in code if line and (not line.startswith(".") or re.match(r"\.LBB\S*:$", line))]
+    labels = {line[:-1]: i for i, line in enumerate(code) if line.endswith(":")}
+    found = []
+    for start, line in enumerate(code):
+        if not line.startswith("v_"):
+            continue
+        operands = line.split(None, 1)[1].split(",") if " " in line or "\t" in line else []
+        written = scalars(operands[0]) if operands else set()
+        if len(operands) > 1 and re.match(r"v_(add|sub|subrev|addc|subb|subbrev)_co|v_div_scale|v_mad_[iu]64", line):
+            written |= scalars(operands[1])
+        if not written:
+            continue
+        paths, seen = [(start + 1, 0, frozenset(written))], set()
+        while paths:
+            at, states, live = paths.pop()
+            if at >= len(code) or states >= needed or not live or (at, states, live) in seen:
+                continue
+            seen.add((at, states, live))
+            here = code[at]
+            if here.endswith(":"):
+                paths.append((at + 1, states, live))
+                continue
+            if re.match(r"(buffer|global|flat|scratch|tbuffer)_", here) and scalars(here) & live:
+                found.append(f"{line} ... {here}, {states} wait states")
+            nop = re.match(r"s_nop (\d+)", here)
+            after = states + (int(nop.group(1)) + 1 if nop else 1)
+            jump = re.match(r"s_c?branch\S*\s+(\.LBB\S+)", here)
+            if jump:
+                paths.append((labels[jump.group(1)], after, live))
+            if re.match(r"s_(branch|endpgm|setpc)", here):
+                continue
+            if here.startswith("s_") and not re.match(r"s_(cmp|bitcmp|nop|waitcnt|barrier|cbranch|setprio|sleep|store)", here):
+                live = live - scalars(here.split(None, 1)[1].split(",")[0]) if len(here.split(None, 1)) > 1 else live
+            paths.append((at + 1, after, live))
+    return found
+
+
+def test_scalar_operands_of_memory_instructions_are_written_early_enough(compiled):
+    """Five wait states between a vector instruction that writes a scalar register (v_readlane brings back a spilled one) and
+    a vector memory instruction that reads it."""
+    planted = ("v_readlane_b32 s1, v190, 26\ns_mov_b32 m0, s93\ns_nop 0\nbuffer_load_dwordx4 v0, s[8:11], s1 offen lds\n"
+               "v_readfirstlane_b32 s4, v2\ns_nop 4\nbuffer_load_dword v1, s[4:7], 0 offen\n"
+               "v_readlane_b32 s9, v190, 2\ns_cbranch_vccz .LBB0_1\ns_endpgm\n.LBB0_1:\nglobal_load_dword v1, v2, s[8:9]\n"
+               "v_readlane_b32 s9, v190, 2\ns_mov_b64 s[8:9], s[2:3]\nglobal_load_dword v1, v2, s[8:9]\ns_endpgm\n")
+    assert [f.rsplit(", ", 1)[1] for f in early_scalar_reads(planted)] == ["2 wait states", "1 wait states"]
+    assert len(re.findall(r"buffer_load_dword.* lds", compiled[1])) > 100
+    assert not early_scalar_reads(compiled[1])
