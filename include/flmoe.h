@@ -384,7 +384,9 @@ int fl_moe_combine_reduce(fl_moe_ctx *ctx, int rank_begin, int rank_count, const
  * Rows are [N][expert_capacity_rows][width], weights [E][out][in] (expert e = d * E/N + j), all contiguous, bf16 unless
  * said otherwise, 16-byte aligned; widths are 8..2^20 and multiples of 8, of 128 where they hold e4m3 blocks
  * (FL_ERR_ALIGNMENT).  An output may not overlap an input, except where said.
- * Products are summed in fp32 (the order is the kernel's own, the same from run to run) and rounded once. */
+ * Products are summed in fp32 and rounded once.  The order is the kernel's own: it goes by the configuration, the widths, the
+ * expert, the output's features, the expert's number of rows and the row's place among them, so a result is the same bit for
+ * bit from run to run, for all ranks at once or part of them, and whatever rows the other experts have. */
 #define FL_ACT_SILU 0 /* v / (1 + e^-v)                                              */
 #define FL_ACT_GELU 1 /* its tanh form: v / (1 + e^(-2 sqrt(2/pi) (v + 0.044715 v^3))) */
 
@@ -392,7 +394,7 @@ int fl_moe_combine_reduce(fl_moe_ctx *ctx, int rank_begin, int rank_count, const
  * x [N][cap][hidden], w [E][2 * inter][hidden]: Wg, then Wu; h [N][cap][inter].
  * pre (may be NULL): keeps both pre-activations x Wg^T, x Wu^T for the backward pass, [N][cap][2 * inter]: bf16, or with
  * pre_scales (fp32 [N][cap][2 * inter / 128], needs inter % 128 == 0) e4m3 codes in blocks of 128 by the rule of
- * FL_DTYPE_E4M3_BLOCK128, half the memory.  h does not depend on how they are kept. */
+ * FL_DTYPE_E4M3_BLOCK128, half the memory.  h is the same bit for bit however they are kept. */
 int fl_moe_expert_gated(const fl_moe_config *cfg /*host*/, int rank_begin, int rank_count, const int32_t *expert_off,
                         const int32_t *tokens_per_expert, int inter, int activation, const void *x, const void *w,
                         void *h, void *pre, float *pre_scales, void *stream);

@@ -241,9 +241,11 @@ struct Tile {
         Place tile;
         int k, n_b, steps;                         // contraction; rows of operand b; steps
         // Few rows: one unit of B.  The weights are then read once and their reading is what takes time, and where rows are
-        // a power of two apart one step's loads all fall on a few memory channels.  So workgroups begin at different steps and
+        // a power of two apart one step's loads all fall on a few memory channels.  So tiles begin at different steps and
         // wrap round: 128 experts of 2 x 768 x 2048 at 16 rows 196 -> 153 us.  (With more rows it would part the
-        // workgroups that share operands: 487 -> 499 us.)
+        // workgroups that share operands: 487 -> 499 us.)  Where a tile begins goes by its expert and its 128 features alone,
+        // one step on from the 128 before, so that a sum's order is the same whatever tiles, grid, ranks or other experts'
+        // rows there are (spread over the steps by the golden section instead: 141.3 -> 143.9 us).
         bool few;
         int shift;
         using Turned = std::integral_constant<bool, true>;
@@ -275,7 +277,7 @@ struct Tile {
             n_b = FORM == kWeightGradient ? P.other : rows.n;
             steps = (int)(((long long)k * size + kStep - 1) / kStep);
             few = kHalves == 1 || n_b - r0 <= kUnitRows;
-            shift = (int)((long long)blockIdx.x * steps / gridDim.x);
+            shift = steps > 0 ? (e * ((P.features + 127) / 128) + f0 / 128) % steps : 0;
             depth = wave * 4 + (l >> 4);
             const int column = ((l & 15) ^ spread(depth)) * 8;
 #pragma unroll

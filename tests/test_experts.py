@@ -901,3 +901,54 @@ def test_no_backward_pass_of_what_was_not_kept():
     with pytest.raises(flmoe.FlMoeError):
         ex.backward(ex.y, w, v, torch.empty_like(w), torch.empty_like(v))
     sh.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows,hidden", [(16, 2056), (40, 2056), (16, 1024), (128, 1096)])
+def test_a_sums_order_goes_by_the_expert_and_its_rows_alone(rows, hidden):
+    """Tiles of few rows begin their sums at different steps of the contraction.  Where goes by the expert and the features: not
+    by what is kept for the backward pass, by the ranks that a call is for, or by the other experts' rows."""
+    n, el, inter = 8, 16, 256
+    counts = [[max(0, rows - (7 * j + 3 * d) % 5) for j in range(el)] for d in range(n)]
+    counts[2][3], counts[5][0] = 0, 1
+    L = Layer(counts, hidden)
+    assert abs(L.cfg.max_tokens // el - rows) <= 4           # the mean that the tile is chosen by
+    x, w, v = L.rows(hidden), L.weights(2 * inter, hidden), L.weights(hidden, inter)
+    wide = -(-hidden // 128) * 128
+    (x8, xs), (w8, ws, w64) = e4m3_rows(L, wide), e4m3_weights(L, inter, wide)
+
+    def run(ranges, keep, loads):
+        h, y, y8 = L.unwritten(inter), L.unwritten(hidden), L.unwritten(inter)
+        pre = {"nothing": None, "bf16": L.unwritten(2 * inter), "e4m3": L.unwritten(2 * inter, torch.uint8)}[keep]
+        scales = L.unwritten(2 * inter // 128, torch.float32) if keep == "e4m3" else None
+        for begin, count in ranges:
+            at = (L.cfg, begin, count, L.expert_off, loads)
+            flmoe.fl_moe_expert_gated(*at, inter, 0, x, w, h, pre, scales)
+            flmoe.fl_moe_expert_product(*at, inter, hidden, h, v, y)
+            flmoe.fl_moe_expert_product_e4m3(*at, wide, inter, x8, xs, w8, ws, y8)
+        return h, y, y8
+    whole = run([(0, n)], "nothing", L.loads)
+    want, tol = ({k: {} for k in ("h", "y", "y8")} for _ in range(2))
+    for d, j in L.experts():
+        at, e = L.span(d, j), d * el + j
+        _, _, h64, dh = gated64(x[d, at].double(), w[e].double(), 0)
+        want["h"][d, j], tol["h"][d, j] = h64, h64.abs() * BF16 + (1 + BF16) * dh + TINY
+        he, ve = whole[0][d, at].double(), v[e].double()
+        want["y"][d, j] = he @ ve.T
+        tol["y"][d, j] = want["y"][d, j].abs() * BF16 + (1 + BF16) * inter * U * (he.abs() @ ve.abs().T) + TINY
+        x64 = dequantised(x8[d, at], xs[d, at])
+        want["y8"][d, j] = x64 @ w64[e].T
+        tol["y8"][d, j] = want["y8"][d, j].abs() * BF16 + (1 + BF16) * (sums(wide) * U * (x64.abs() @ w64[e].abs().T) + cut(x64, w64[e])) + TINY
+    for name, got in zip(("h", "y", "y8"), whole):
+        L.check_rows(got, want[name], tol[name], name)
+    for keep in ("nothing", "bf16", "e4m3"):
+        for got, first in zip(run([(0, n)], keep, L.loads), whole):
+            assert torch.equal(got, first), keep
+        for got, first in zip(run([(r, 1) for r in range(n)], keep, L.loads), whole):
+            assert torch.equal(got, first), (keep, "rank by rank")
+    fewer = L.loads.clone()                                  # the other experts' rows: half of the experts have none
+    fewer.view(-1)[::2] = 0
+    for got, first in zip(run([(0, n)], "nothing", fewer), whole):
+        for d, j in L.experts():
+            if int(fewer[d, j]):
+                assert torch.equal(got[d, L.span(d, j)], first[d, L.span(d, j)]), (d, j)
