@@ -79,7 +79,7 @@ extern "C" {
 /* OCP E4M3 (finite-only) bytes plus one fp32 scale per 128 elements, quantised
  * by dispatch_send (workload of section Kernel Microbenchmarks: 7168 fp8 values
  * and 56 fp32 scaling factors per token).  Per block of 128: scale = max|x| / 448
- * (1 when the maximum is 0), code = e4m3(x / scale), round to nearest even,
+ * (1 when that is 0), code = e4m3(x / scale), round to nearest even,
  * saturating; both divisions IEEE fp32.  Non-finite inputs (the paper is silent; the
  * rule is applied as written): a NaN is skipped by the maximum and becomes the NaN
  * code 0x7f with its own sign, its neighbours are quantised as if it were absent; an

@@ -81,7 +81,11 @@ __device__ inline float activate(int act, float v, float *slope) {
 
 // Codes of four values of an e4m3 block (see FL_DTYPE_E4M3_BLOCK128): rounded to nearest even, saturating; what is NaN
 // over the scale (a NaN, or an Inf in a block whose scale it made infinite) becomes the NaN code with the value's sign.
-__device__ inline float block_scale(float amax) { return amax == 0.0f ? 1.0f : __fdiv_rn(amax, 448.0f); }
+// (A maximum below about 3e-43, which no bf16 row has but an fp32 product may, over 448 is 0: such a block is zeros too.)
+__device__ inline float block_scale(float amax) {
+    const float scale = __fdiv_rn(amax, 448.0f);
+    return scale == 0.0f ? 1.0f : scale;
+}
 __device__ inline unsigned e4m3_codes(const float *v, float scale) {
     float q[4];
     bool odd = false;

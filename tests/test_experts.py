@@ -952,3 +952,23 @@ def test_a_sums_order_goes_by_the_expert_and_its_rows_alone(rows, hidden):
         for d, j in L.experts():
             if int(fewer[d, j]):
                 assert torch.equal(got[d, L.span(d, j)], first[d, L.span(d, j)]), (d, j)
+
+
+@pytest.mark.gpu
+def test_blocks_of_values_too_small_for_a_scale_are_zeros():
+    """The largest product of a block is 2^-145: over 448 it is 0, no scale that its zeros could be divided by."""
+    hidden = inter = 128
+    L = Layer([[3]], hidden)
+    x = torch.zeros((1, L.cap, hidden), device="cuda")
+    w = torch.zeros((1, 2 * inter, hidden), device="cuda")
+    x[0, 0, 0] = w[0, 5, 0] = w[0, inter + 5, 0] = 1.0
+    x, w = x.to(torch.float8_e4m3fn), w.to(torch.float8_e4m3fn)
+    xs = torch.ones((1, L.cap, 1), device="cuda")
+    ws = torch.tensor([2.0 ** -70, 2.0 ** -74], device="cuda").view(1, 2, 1)     # silu(2^-70) = 2^-71
+    h, hs, y = L.unwritten(inter, torch.uint8), L.unwritten(1, torch.float32), L.unwritten(hidden)
+    flmoe.fl_moe_expert_gated_e4m3(*L.at, inter, 0, x, xs, w, ws, h, hs)
+    assert hs[0, :3, 0].tolist() == [1.0, 1.0, 1.0]
+    assert not bool((h[0, :3] & 0x7f).any())
+    v = torch.ones((1, hidden, inter), device="cuda").to(torch.float8_e4m3fn)
+    flmoe.fl_moe_expert_product_e4m3(*L.at, inter, hidden, h, hs, v, torch.ones((1, 1, 1), device="cuda"), y)
+    assert not bool(y[0, :3].any())
