@@ -608,6 +608,17 @@ class MoEExperts:
             self.dpre = rows(2 * inter) if eights else self.pre
             self.dh, self.dx = rows(inter), rows(shuffle.H)
             self.tables = [torch.zeros((shuffle.N, n), dtype=torch.int32, device=shuffle.device) for n in (shuffle.El + 1, shuffle.El)]
+            # of each rank: whether there is something kept for a backward pass; None once a forward pass was captured, whose
+            # replays are not seen here
+            self._kept = [False] * shuffle.N
+
+    def _stream(self, stream):
+        if stream is None:
+            return torch.cuda.current_stream(self.shuffle.device)
+        return stream if hasattr(stream, "cuda_stream") else torch.cuda.ExternalStream(int(stream), device=self.shuffle.device)
+
+    def _keep(self, rb, rc, kept):
+        self._kept[rb:rb + rc] = [None if was is None or kept is None else kept for was in self._kept[rb:rb + rc]]
 
     def _at(self, ranks):
         rb, rc = self.shuffle._ranks(ranks)
@@ -619,11 +630,10 @@ class MoEExperts:
         if (x_scales is not None) != (x is not None and self.e4m3):
             raise FlMoeError(FL_ERR_INVALID_ARG, "MoEExperts.forward: other rows of e4m3 come with their scales")
         if self.training:
-            on = torch.cuda.current_stream(sh.device) if stream is None else stream
-            if not hasattr(on, "cuda_stream"):
-                on = torch.cuda.ExternalStream(int(on), device=sh.device)
-            with torch.cuda.stream(on):
-                rb, rc = sh._ranks(ranks)                # only theirs: the others' may be on their way on other streams
+            rb, rc = sh._ranks(ranks)                    # only theirs: the others' may be on their way on other streams
+            with torch.cuda.stream(self._stream(stream)):
+                captured = torch.cuda.is_current_stream_capturing()
+                self._keep(rb, rc, None if captured else False)
                 for mine, now in zip(self.tables, (sh.layout_tables()[t] for t in ("expert_off", "G"))):
                     mine[rb:rb + rc].copy_(now[rb:rb + rc])
         else:
@@ -636,20 +646,31 @@ class MoEExperts:
         else:
             fl_moe_expert_gated(*at, self.inter, self.activation, x, w_in, self.h, self.pre, self.pre_scales, stream)
             fl_moe_expert_product(*at, self.inter, sh.H, self.h, w_out, self.y, stream)
+        if self.training:
+            self._keep(rb, rc, True)
         return self.y
 
     def backward(self, dy, w_in, w_out, dw_in, dw_out, x=None, ranks=None, stream=None):
-        """The rows' gradient; the weights' go to dw_in and dw_out.  Once per forward: with bf16 the kept pre-activations are
-        gone then.  x: the rows that forward had."""
+        """The rows' gradient; the weights' go to dw_in and dw_out.  x: the rows that forward had.  Once per forward of these
+        ranks with keep="bf16": the kept pre-activations are gone then, another call is refused.  (Calls captured into a graph,
+        and those behind a captured forward, are not checked: their replays are the caller's to keep in turn.)"""
         if not self.training:
             raise FlMoeError(FL_ERR_INVALID_ARG, "MoEExperts.backward: nothing was kept, training was not asked for")
         sh, at = self.shuffle, self._at(ranks)
+        rb, rc = at[1:3]
+        with torch.cuda.stream(self._stream(stream)):
+            captured = torch.cuda.is_current_stream_capturing()
+        if not captured and False in self._kept[rb:rb + rc]:
+            raise FlMoeError(FL_ERR_INVALID_ARG, "MoEExperts.backward: nothing is kept of these ranks' rows: no forward pass, or its "
+                             "backward pass has been")
         x = sh.expert_x if x is None else x
         again = self.h if self.keep == "e4m3" else None
         fl_moe_expert_product_backward(*at, self.inter, sh.H, self.h, w_out, dy, self.dh, None if again is not None else dw_out,
                                        stream)
         fl_moe_expert_gated_backward(*at, self.inter, self.activation, x, w_in, self.pre, self.pre_scales, self.dh, self.dpre,
                                      self.dx, dw_in, again, stream)
+        if not captured and self.dpre is self.pre:
+            self._keep(rb, rc, False)
         if again is not None:
             fl_moe_expert_product_backward(*at, self.inter, sh.H, again, None, dy, None, dw_out, stream)
         return self.dx

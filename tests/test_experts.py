@@ -972,3 +972,84 @@ def test_blocks_of_values_too_small_for_a_scale_are_zeros():
     v = torch.ones((1, hidden, inter), device="cuda").to(torch.float8_e4m3fn)
     flmoe.fl_moe_expert_product_e4m3(*L.at, inter, hidden, h, hs, v, torch.ones((1, 1, 1), device="cuda"), y)
     assert not bool(y[0, :3].any())
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("keep", ["bf16", "e4m3"])
+def test_a_backward_pass_needs_what_a_forward_pass_kept(keep):
+    """With bf16 it takes the place of what was kept: a second one, of all ranks or of one that has had its own, is refused.  What
+    was kept in 8 bits stays."""
+    wl, inp, dev, harness = layer_inputs()
+    sh = harness.make_shuffle(inp)
+    ex, (w, v) = harness.make_experts(sh, 128, training=True, keep=keep)
+    dy = torch.randn(ex.y.shape, generator=torch.Generator(device="cuda").manual_seed(2), device="cuda").to(torch.bfloat16)
+
+    def backward(ranks=None):
+        dw, dv = torch.zeros_like(w), torch.zeros_like(v)
+        dx = ex.backward(dy, w, v, dw, dv, ranks=ranks)
+        return dw, dv, dx.clone()
+
+    def refused(ranks=None):
+        with pytest.raises(flmoe.FlMoeError) as e:
+            backward(ranks)
+        assert e.value.code == INVALID
+
+    def used(dx):
+        off, load = (t.cpu() for t in ex.tables)
+        return torch.cat([dx[d, int(off[d, j]):int(off[d, j] + load[d, j])] for d in range(sh.N) for j in range(sh.El)])
+    refused()                                                # no forward pass yet
+    harness.run_layer(sh, ex, (w, v), dev)
+    with pytest.raises(flmoe.FlMoeError):                    # a call that is refused for its tensors takes nothing away
+        ex.backward(dy, w, v, torch.zeros_like(w)[:1], torch.zeros_like(v))
+    dw, dv, dx = backward()
+    if keep == "e4m3":
+        for a, b in zip(backward()[:2], (dw, dv)):
+            assert torch.equal(a, b)
+        sh.close()
+        return
+    refused()
+    ex.forward(w, v, ranks=(1, 2))
+    refused()
+    refused((0, 2))
+    parts = backward((2, 1))
+    refused((2, 1))
+    refused((1, 2))
+    for a, b in zip(parts[:2], (dw, dv)):
+        assert torch.equal(a[2 * sh.El:3 * sh.El], b[2 * sh.El:3 * sh.El])
+    backward((1, 1))
+    # the forward pass from a graph: its replays are not seen, so nothing is refused
+    ex.forward(w, v)
+    backward()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        ex.forward(w, v)
+    for _ in range(3):
+        graph.replay()
+        again = backward()
+        torch.cuda.synchronize()
+        assert torch.equal(again[0], dw) and torch.equal(again[1], dv) and torch.equal(used(again[2]), used(dx))
+    sh.close()
+
+
+@pytest.mark.gpu
+def test_both_passes_of_the_experts_in_one_graph():
+    wl, inp, dev, harness = layer_inputs()
+    sh = harness.make_shuffle(inp)
+    ex, (w, v) = harness.make_experts(sh, 128, training=True)
+    harness.run_layer(sh, ex, (w, v), dev)
+    dy, dw, dv = ex.y.clone(), torch.zeros_like(w), torch.zeros_like(v)
+    ex.backward(dy, w, v, dw, dv)
+    want = dw.clone(), dv.clone()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        ex.forward(w, v)
+        ex.backward(dy, w, v, dw, dv)
+    for _ in range(3):
+        dw.fill_(77)
+        dv.fill_(77)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(dw, want[0]) and torch.equal(dv, want[1])
+    sh.close()
