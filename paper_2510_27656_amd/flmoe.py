@@ -589,7 +589,9 @@ class MoEExperts:
 
     def __init__(self, shuffle, inter, activation="silu", training=False, keep="bf16"):
         self.shuffle, self.inter, self.training, self.keep = shuffle, inter, training, keep
-        self.activation = {"silu": FL_ACT_SILU, "gelu": FL_ACT_GELU}[activation]
+        if activation not in ("silu", "gelu"):
+            raise FlMoeError(FL_ERR_INVALID_ARG, f"MoEExperts: activation is silu or gelu, got {activation!r}")
+        self.activation = FL_ACT_SILU if activation == "silu" else FL_ACT_GELU
         self.e4m3 = shuffle.expert_scales is not None
         if keep not in ("bf16", "e4m3") or (training and self.e4m3):
             raise FlMoeError(FL_ERR_INVALID_ARG, "MoEExperts: rows of e4m3 have no backward pass; keep is bf16 or e4m3")

@@ -1053,3 +1053,13 @@ def test_both_passes_of_the_experts_in_one_graph():
         torch.cuda.synchronize()
         assert torch.equal(dw, want[0]) and torch.equal(dv, want[1])
     sh.close()
+
+
+@pytest.mark.gpu
+def test_other_activations_are_refused():
+    wl, inp, dev, harness = layer_inputs()
+    sh = harness.make_shuffle(inp)
+    with pytest.raises(flmoe.FlMoeError) as e:
+        flmoe.MoEExperts(sh, 128, activation="relu")
+    assert e.value.code == INVALID
+    sh.close()
