@@ -1063,3 +1063,47 @@ def test_other_activations_are_refused():
         flmoe.MoEExperts(sh, 128, activation="relu")
     assert e.value.code == INVALID
     sh.close()
+
+
+def expert_rows(sh, wl, inp, dev, off, load):
+    """The routing weights of the expert rows, and [(s, t, rank, rows)] of every expert's pairs."""
+    weights, places = torch.zeros((sh.N, sh.expert_capacity_rows), device="cuda"), []
+    for e, p in tokens_by_expert(wl, inp).items():
+        d, j = e // sh.El, e % sh.El
+        assert len(p) == int(load[d, j])
+        s, t, k = (torch.tensor(c, device="cuda") for c in zip(*p))
+        rows = slice(int(off[d, j]), int(off[d, j]) + len(p))
+        weights[d, rows] = dev["weights"][s, t, k]
+        places.append((s, t, d, rows))
+    return weights, places
+
+
+@pytest.mark.gpu
+def test_a_training_step_of_a_layer_with_partial_sums():
+    """The tokens' gradients come back as one row of each rank: the rank's sum of fp32, rounded, then the sum of those."""
+    wl, inp, dev, harness = layer_inputs()
+    sh = harness.make_shuffle(inp, partial_sums=True)
+    ex, (w, v) = harness.make_experts(sh, 128, training=True)
+    harness.run_layer(sh, ex, (w, v), dev)
+    x, (off, load) = sh.expert_x.clone(), (t.cpu() for t in ex.tables)
+    row_weights, places = expert_rows(sh, wl, inp, dev, off, load)
+    dout = torch.randn(sh.out.shape, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda").to(torch.bfloat16)
+    dw, dv = torch.full_like(w, 77), torch.full_like(v, 77)
+    dx = harness.run_layer_backward(sh, ex, (w, v), (dw, dv), dev, x, dout, row_weights, torch.ones_like(dev["weights"]))
+    assert sh.status() == 0
+    for (s, t, d, rows), e in zip(places, tokens_by_expert(wl, inp)):
+        dy = (dout[s, t].float() * row_weights[d, rows, None]).to(torch.bfloat16).double()
+        h, n = ex.h[d, rows].double(), len(s)
+        check(dv[e], dy.T @ h, (dy.T @ h).abs() * BF16 + (1 + BF16) * n * U * (dy.abs().T @ h.abs()) + TINY, f"dw_out of {e}")
+        dp, xe = ex.dpre[d, rows].double(), x[d, rows].double()
+        check(dw[e], dp.T @ xe, (dp.T @ xe).abs() * BF16 + (1 + BF16) * n * U * (dp.abs().T @ xe.abs()) + TINY, f"dw_in of {e}")
+    of_rank = torch.zeros((sh.N, *dx.shape), dtype=torch.float64, device="cuda")
+    size = torch.zeros(dx.shape, dtype=torch.float64, device="cuda")
+    for s, t, d, rows in places:
+        of_rank[d].index_put_((s, t), ex.dx[d, rows].double(), accumulate=True)
+        size.index_put_((s, t), ex.dx[d, rows].double().abs(), accumulate=True)
+    off = of_rank.abs().sum(0) * BF16 + 2 * wl.top_k * U * size              # the ranks' sums are rounded
+    for r in range(wl.n_ranks):
+        n, want = int(inp.num_tokens[r]), of_rank.sum(0)[r]
+        check(dx[r, :n], want[:n], want[:n].abs() * BF16 + (1 + BF16) * off[r, :n] + TINY, f"dx of rank {r}")
+    sh.close()
