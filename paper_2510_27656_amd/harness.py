@@ -190,10 +190,10 @@ def run_layer_backward(sh: flmoe.MoEShuffle, ex: flmoe.MoEExperts, weights, grad
     row of it times the row's routing weight is the gradient of y, and the rows' gradients come back the way the replies
     came (combine with weights of one).  x: a copy of the rows that the forward pass had in expert_x, which the gradient's
     rows overwrite; row_weights [N][capacity] fp32: the routing weight of each expert row; ones: dev["weights"]' shape.
-    Returns the tokens' gradient; the routing weights' own (per pair, the product of y and the gradient's row) is the
-    caller's."""
+    Returns the tokens' gradient, zeros for those that a rank does not have; the routing weights' own (per pair, the product
+    of y and the gradient's row) is the caller's."""
     sh.layout(dev["indices"], dev["num_tokens"])
     sh.dispatch_send(dout, weights=ones if sh.partial_sums else None)
     dy = (sh.dispatch_recv().float() * row_weights[..., None]).to(torch.bfloat16)
     sh.combine_send(ex.backward(dy, *weights, *grads, x=x))
-    return sh.combine_reduce(ones, out=torch.empty_like(sh.out))
+    return sh.combine_reduce(ones, out=torch.zeros_like(sh.out))

@@ -1107,3 +1107,18 @@ def test_a_training_step_of_a_layer_with_partial_sums():
         n, want = int(inp.num_tokens[r]), of_rank.sum(0)[r]
         check(dx[r, :n], want[:n], want[:n].abs() * BF16 + (1 + BF16) * off[r, :n] + TINY, f"dx of rank {r}")
     sh.close()
+
+
+@pytest.mark.gpu
+def test_tokens_that_a_rank_does_not_have_get_no_gradient():
+    wl, inp, dev, harness = layer_inputs()
+    sh = harness.make_shuffle(inp)
+    ex, (w, v) = harness.make_experts(sh, 128, training=True)
+    harness.run_layer(sh, ex, (w, v), dev)
+    row_weights, _ = expert_rows(sh, wl, inp, dev, *(t.cpu() for t in ex.tables))
+    x, dout, ones = sh.expert_x.clone(), torch.zeros_like(sh.out), torch.ones_like(dev["weights"])
+    before = [torch.full_like(sh.out, 77) for _ in range(4)]                 # what the allocator hands out next
+    del before
+    dx = harness.run_layer_backward(sh, ex, (w, v), (torch.empty_like(w), torch.empty_like(v)), dev, x, dout, row_weights, ones)
+    assert min(inp.num_tokens) < wl.tokens and not bool(dx.any())
+    sh.close()
