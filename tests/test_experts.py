@@ -1122,3 +1122,87 @@ def test_tokens_that_a_rank_does_not_have_get_no_gradient():
     dx = harness.run_layer_backward(sh, ex, (w, v), (torch.empty_like(w), torch.empty_like(v)), dev, x, dout, row_weights, ones)
     assert min(inp.num_tokens) < wl.tokens and not bool(dx.any())
     sh.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,el,mean", [(4, 256, 4), (4, 256, 40), (40, 25, 100), (3, 171, 30)])
+def test_more_experts_than_a_workgroup_has_threads(n, el, mean):
+    """The counts are scanned in turns of 256 or 512; the last experts, alone and with all others, have their own rows."""
+    in_, out = 128, 136
+    counts = [[(j * 7 + d * 3) % (2 * mean + 1) for j in range(el)] for d in range(n)]
+    counts[-1][-1] = mean + 300                              # more than one tile behind all others
+    L = Layer(counts, in_)
+    assert abs(L.cfg.max_tokens // el - mean) <= 15          # the mean that the tile is chosen by
+    x, w, dy = L.rows(in_), L.weights(out, in_), L.rows(out)
+    y, dx, dw, part = L.unwritten(out), L.unwritten(in_), torch.full_like(w, 77), L.unwritten(out)
+    flmoe.fl_moe_expert_product(*L.at, in_, out, x, w, y)
+    flmoe.fl_moe_expert_product_backward(*L.at, in_, out, x, w, dy, dx, dw)
+    flmoe.fl_moe_expert_product(L.cfg, n - 1, 1, L.expert_off, L.loads, in_, out, x, w, part)
+    assert torch.equal(part[n - 1], y[n - 1]) and bool((part[:n - 1] == 77).all())
+    for d in range(n):                                       # a rank's experts in one batch, padded
+        most = max(max(counts[d]), 1)
+        at = torch.tensor([[L.off[d][j] + min(r, max(counts[d][j] - 1, 0)) for r in range(most)] for j in range(el)], device="cuda")
+        there = (torch.arange(most, device="cuda")[None] < L.loads[d][:, None])[..., None]
+        take = lambda rows: rows[d][at].double().masked_fill(~there, 0)
+        xe, de, we = take(x), take(dy), w[d * el:(d + 1) * el].double()
+        for got, a, b, steps in ((take(y), xe, we.transpose(1, 2).contiguous(), in_), (take(dx), de, we, out),
+                                 (dw[d * el:(d + 1) * el].double(), de.transpose(1, 2).contiguous(), xe, most)):
+            want, size = torch.bmm(a, b), torch.bmm(a.abs(), b.abs())
+            check(got, want, want.abs() * BF16 + (1 + BF16) * steps * U * size + TINY, f"rank {d}")
+    for got in (y, dx):
+        assert bool((got[~L.used] == 77).all())
+
+
+@pytest.mark.gpu
+def test_codes_and_scales_that_are_not_finite_stay_in_their_rows():
+    """NaN codes and infinite or NaN scales of rows that are in use: the row is NaN where they enter, its neighbours are not."""
+    counts, in_, out = [[20, 3, 140]], 384, 264
+    L = Layer(counts, in_)
+    (x, xs), (w, ws, _) = e4m3_rows(L, in_), e4m3_weights(L, out, in_)
+    y, clean = L.unwritten(out), L.unwritten(out)
+    flmoe.fl_moe_expert_product_e4m3(*L.at, in_, out, x, xs, w, ws, clean)
+    x.view(torch.uint8)[0, 4, 300], x.view(torch.uint8)[0, 160, 0] = 0x7f, 0xff
+    xs[0, 19, 2], xs[0, 21, 0] = math.nan, math.inf
+    flmoe.fl_moe_expert_product_e4m3(*L.at, in_, out, x, xs, w, ws, y)
+    bad = [4, 160, 19, 21]
+    fine = [r for r in range(163) if r not in bad]
+    assert torch.equal(y[0, fine], clean[0, fine])
+    assert bool(y[0, [4, 160, 19]].isnan().all()) and not bool(y[0, 21].isfinite().any())
+    # in the weights: the features whose codes or block they are in, of that expert
+    w.view(torch.uint8)[1, 200, 17] = 0x7f
+    ws[2, 2, 1] = math.inf                                   # features 256 to 263
+    x, xs = e4m3_rows(L, in_)
+    flmoe.fl_moe_expert_product_e4m3(*L.at, in_, out, x, xs, w, ws, y)
+    assert bool(y[0, :20].isfinite().all())
+    one = torch.arange(out, device="cuda") == 200
+    assert bool(y[0, 20:23, one].isnan().all()) and bool(y[0, 20:23, ~one].isfinite().all())
+    assert bool(y[0, 23:163, :256].isfinite().all()) and not bool(y[0, 23:163, 256:].isfinite().any())
+    # the gated block answers with blocks of NaN codes there, finite ones elsewhere
+    hidden, inter = 384, 256
+    (x, xs), (w, ws, _) = e4m3_rows(L, hidden), e4m3_weights(L, 2 * inter, hidden)
+    x.view(torch.uint8)[0, 7, 100] = 0x7f
+    h, hs = L.unwritten(inter, torch.uint8), L.unwritten(inter // 128, torch.float32)
+    flmoe.fl_moe_expert_gated_e4m3(*L.at, inter, 0, x, xs, w, ws, h, hs)
+    assert bool(((h[0, 7] & 0x7f) == 0x7f).all()) and bool((hs[0, 7] == 1).all())
+    rest = [r for r in range(163) if r != 7]
+    assert not bool(((h[0, rest] & 0x7f) == 0x7f).any()) and bool(hs[0, rest].isfinite().all())
+
+
+@pytest.mark.gpu
+def test_each_gradient_of_the_gated_block_alone():
+    """dx, dw, both or neither: the same bits; dpre is there each time."""
+    counts, hidden, inter = [[40, 0, 300], [129, 1, 7]], 264, 136
+    L = Layer(counts, hidden)
+    x, w, dh, pre = L.rows(hidden), L.weights(2 * inter, hidden), L.rows(inter), L.rows(2 * inter)
+
+    def run(want_dx, want_dw):
+        dpre, dx, dw = L.unwritten(2 * inter), L.unwritten(hidden), torch.full_like(w, 77)
+        flmoe.fl_moe_expert_gated_backward(*L.at, inter, 1, x if want_dw else None, w if want_dx else None, pre, None, dh, dpre,
+                                           dx if want_dx else None, dw if want_dw else None)
+        return dpre, dx, dw
+    both = run(True, True)
+    for want_dx, want_dw in ((True, False), (False, True), (False, False)):
+        dpre, dx, dw = run(want_dx, want_dw)
+        assert torch.equal(dpre, both[0])
+        assert torch.equal(dx, both[1]) if want_dx else bool((dx == 77).all())
+        assert torch.equal(dw, both[2]) if want_dw else bool((dw == 77).all())
