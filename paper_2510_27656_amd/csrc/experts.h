@@ -64,13 +64,20 @@ inline int launched() { return hipGetLastError() == hipSuccess ? FL_OK : FL_ERR_
 
 // mean: rows an expert would have if the tokens of the configuration were spread evenly.
 // Experts of few rows are bound by the reading of their weights; smaller tiles leave less of the machine idle at the beginning
-// and the end of each and spread few experts over more compute units.  us of both products of one call, 128 experts of
-// 2 x 768 x 2048 in bf16, tiles of 256, 64 and 32 rows: 16 rows 156 / 89, 146 / 80 and 143 / 77; 48 rows 160 / 103, 152 / 91;
-// 64 rows 164 / 107, 156 / 94; 128 rows 185 / 126, 217 / 131; e4m3, 64 experts of 7168 x 2048, the product behind, 4 rows 174, 185,
-// 159.  The counts scatter round their mean, so that an expert hardly ever has two tiles where one was meant:
-constexpr long long kRowsFor32 = 20, kRowsFor64 = 48;
+// and the end of each and spread few experts over more compute units.  A real routing scatters the counts round their mean, and an
+// expert with one row more than a tile has its weights read twice, which is why the lines lie below 32 and 64.  us with a random
+// top 8 of 128 experts of 2 x 768 x 2048 in bf16, tiles of 32, 64 and 256 rows, gated block and product behind:
+//   mean 16  140 / 78,  142 / 78,  144 / 86      40  182 / 103, 146 / 88, 148 / 88
+//        20  154 / 84,  143 / 79,  146 / 86      48  193 / 106, 160 / 96, 151 / 88
+//        32  158 / 92,  146 / 85,  147 / 87      64  212 / 117, 184 / 107, 155 / 91
+// e4m3, the product of 64 experts of 4096 x 2048: 16 rows 104, 110, 113; 24 110, 108, 111; 40 135, 114, 113; 48 141, 121, 114; the
+// gated block there, in tiles of 64 and 256: 40 194, 205; 48 219, 207.
+constexpr long long kRowsFor32 = 16, kRowsFor64 = 40;
 // Workgroups of small tiles on a compute unit: what is on its way to one is best 64 to 96 KB (32 KB each); the third pays where a
-// tile is short (128 experts, e4m3, 768 long: 44 -> 36 us, bf16 2048 long 143 -> 147).
+// tile is short.  us with two and with three, 128 experts, tiles of 32 rows: bf16, 2048 outputs, 512 long 49 and 44, 1024 103 and
+// 102, 1792 166 and 167; e4m3, 4096 outputs, 512 63 and 55, 1024 114 and 108, 2048 200 and 202 (64 experts of
+// 7168 x 2048, both products, 4 rows: 474 and 467).  Tiles of 64 rows: bf16, 512 52 and 48, 768 87 and 88; e4m3 never (768 103 and 118,
+// 2048 223 and 252).
 constexpr int kShortBytes = 2048;
 
 template <int FORM, bool E4M3, bool GATED>
@@ -88,9 +95,9 @@ int launch_tiles(const Groups &G, long long mean, const Product &P, hipStream_t 
                 return go(integral_constant<int, 64>(), integral_constant<int, 128>(), 1);
         }
         if constexpr (!(E4M3 && GATED)) {
-            const int per_unit = P.k * (E4M3 ? 1 : 2) <= kShortBytes ? 3 : 2;
-            if (mean <= kRowsFor32) return go(integral_constant<int, 32>(), integral_constant<int, 64>(), per_unit);
-            if (mean <= kRowsFor64) return go(integral_constant<int, 64>(), integral_constant<int, 64>(), per_unit);
+            const bool small = P.k * (E4M3 ? 1 : 2) <= kShortBytes;
+            if (mean <= kRowsFor32) return go(integral_constant<int, 32>(), integral_constant<int, 64>(), small ? 3 : 2);
+            if (mean <= kRowsFor64) return go(integral_constant<int, 64>(), integral_constant<int, 64>(), small && !E4M3 ? 3 : 2);
         }
     }
     return go(integral_constant<int, 256>(), integral_constant<int, 128>(), 1);
