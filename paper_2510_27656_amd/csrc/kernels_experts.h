@@ -158,8 +158,8 @@ __device__ inline void loads_done_and_barrier() {
 
 // ---------------------------------------------------------------- the tiles
 // 256 features by 256 rows, eight waves, two on each SIMD: 32 accumulators of 16 by 16 outputs a wave, half of what the
-// registers hold; memory is read once for 256 operations a byte.  A step multiplies 128 bytes of the contraction (64 bf16,
-// 128 e4m3).  Both operands of a step come in two units of 16 KB (A0, A1: 128 features each, of a gated tile the gates and
+// registers hold; an operand's byte, once read, serves 128 operations in bf16, 256 in e4m3.  A step multiplies 128 bytes of
+// the contraction (64 bf16, 128 e4m3).  Both operands of a step come in two units of 16 KB (A0, A1: 128 features each, of a gated tile the gates and
 // their ups; B0, B1: 128 rows each), and each wave owns 64 of the features and 32 of the rows of every unit.  A step has
 // two phases; each reads from LDS what the products behind it take, over what has been used up, while the ones before it are
 // under way:
