@@ -427,7 +427,8 @@ int fl_moe_expert_product_backward(const fl_moe_config *cfg /*host*/, int rank_b
  * [N][cap][hidden / 128]; w codes [E][2 * inter][hidden] with one scale per 128 x 128 block, w_scales fp32
  * [E][2 * inter / 128][hidden / 128].  h is answered in e4m3 blocks of 128, quantised from the fp32 result by the rule of
  * FL_DTYPE_E4M3_BLOCK128: codes [N][cap][inter], h_scales [N][cap][inter / 128].
- * Every block's codes are multiplied and summed as they are, and the sum enters an fp32 accumulator times both scales.
+ * Every block's codes are multiplied and summed as they are, and the sum enters an fp32 accumulator times both scales
+ * (times their product, itself an fp32 value: where that leaves the range of normal numbers, so does the block's part).
  * (Within a block the part's matrix instruction adds the products of eight neighbours after cutting each 13 binary
  * places below the largest of the eight; those sums are added in fp32.  It loses less than 7 * 2^-13 of the largest
  * product of eight, in practice a tenth of what the rounding to bf16 does.) */
