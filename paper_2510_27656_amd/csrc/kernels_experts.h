@@ -169,10 +169,10 @@ __device__ inline void loads_done_and_barrier() {
 // units just read are loaded for two steps later.  So with two places for each unit the loads that fill one have a step
 // and a half to arrive, and 64 to 96 KB are on their way to a compute unit all the time.  (Four phases of one quadrant
 // each, a barrier behind each: the row gradient took 6 % longer.)
-// Full tiles with contractions of 7168 and more reach 1290 to 1320 Tflop/s in bf16 (a large library product on this card 1400
-// to 1580), the loop by itself 1350; what begins and ends a tile takes 9 us, as long as six of its steps (32 x 1024 rows, 1024 wide,
-// contractions of 512 to 7168: 82 to 745 us).  e4m3 reaches 1870 to 2000: there the block scales' fused multiplications take about
-// an eighth of the time and the loads into LDS a fifth.
+// Full tiles with contractions of 7168 and more reach 1280 to 1330 Tflop/s in bf16 (a large library product on this card 1400
+// to 1600), the loop by itself 1350; what begins and ends a tile takes 8 us, as long as five of its steps (32 x 1024 rows, 1024
+// wide, contractions of 512 to 7168: 82 to 735 us).  e4m3 reaches 1880 to 2030: there the block scales' fused multiplications
+// take about an eighth of the time and the loads into LDS a fifth.
 constexpr int kStep = 128;                     // bytes of the contraction per step
 constexpr int kXcds = 8;
 
