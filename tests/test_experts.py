@@ -1206,3 +1206,53 @@ def test_each_gradient_of_the_gated_block_alone():
         assert torch.equal(dpre, both[0])
         assert torch.equal(dx, both[1]) if want_dx else bool((dx == 77).all())
         assert torch.equal(dw, both[2]) if want_dw else bool((dw == 77).all())
+
+
+@pytest.mark.gpu
+def test_calls_without_any_rows():
+    """No expert has rows: rows are left as they are, weight gradients are zero."""
+    in_, out = 384, 256
+    L = Layer([[0, 0, 0], [0, 0, 0]], in_)
+    x, w, dy = L.rows(in_), L.weights(out, in_), L.rows(out)
+    y, dx, dw = L.unwritten(out), L.unwritten(in_), torch.full_like(w, 77)
+    flmoe.fl_moe_expert_product(*L.at, in_, out, x, w, y)
+    flmoe.fl_moe_expert_product_backward(*L.at, in_, out, x, w, dy, dx, dw)
+    h, pre, dpre = L.unwritten(out // 2), L.unwritten(out), L.unwritten(out)
+    flmoe.fl_moe_expert_gated(*L.at, out // 2, 0, x, w, h, pre)
+    dv = torch.full_like(w, 77)
+    flmoe.fl_moe_expert_gated_backward(*L.at, out // 2, 0, x, w, pre, None, L.rows(out // 2), dpre, dx, dv)
+    (x8, xs), (w8, ws, _) = e4m3_rows(L, in_), e4m3_weights(L, out, in_)
+    y8, h8, hs = L.unwritten(out), L.unwritten(out // 2, torch.uint8), L.unwritten(1, torch.float32)
+    flmoe.fl_moe_expert_product_e4m3(*L.at, in_, out, x8, xs, w8, ws, y8)
+    flmoe.fl_moe_expert_gated_e4m3(*L.at, out // 2, 1, x8, xs, w8, ws, h8, hs)
+    for left in (y, dx, h, pre, dpre, y8, h8, hs):
+        assert bool((left == 77).all())
+    assert not bool(dw.any()) and not bool(dv.any())
+
+
+@pytest.mark.gpu
+def test_calls_on_several_streams_at_once():
+    """The calls keep nothing and share nothing: three streams of them, of different sizes, run beside each other."""
+    layers, streams = [], [torch.cuda.Stream() for _ in range(3)]
+    for n, (counts, in_, out) in enumerate((([[300, 5], [40, 700]], 1024, 520), ([[16] * 16] * 2, 2056, 256), ([[1200]], 512, 1032))):
+        L = Layer(counts, in_, seed=n)
+        layers.append((L, in_, out, L.rows(in_), L.weights(out, in_), L.rows(out)))
+
+    def run(stream, L, in_, out, x, w, dy, y, dx, dw):
+        for _ in range(4):
+            flmoe.fl_moe_expert_product(*L.at, in_, out, x, w, y, stream=stream)
+            flmoe.fl_moe_expert_product_backward(*L.at, in_, out, x, w, dy, dx, dw, stream=stream)
+
+    def results():
+        return [(L.unwritten(out), L.unwritten(in_), torch.full_like(w, 77)) for L, in_, out, _, w, _ in layers]
+    apart, together = results(), results()
+    for given, got in zip(layers, apart):
+        run(None, *given, *got)
+    torch.cuda.synchronize()
+    for _ in range(3):
+        for stream, given, got in zip(streams, layers, together):
+            run(stream, *given, *got)
+    torch.cuda.synchronize()
+    for one, other in zip(apart, together):
+        for a, b in zip(one, other):
+            assert torch.equal(a, b)
